@@ -1,0 +1,589 @@
+"""Measured calls of the rotary positions and of the 4-bit cache: rotating queries
+and keys, packing a built cache into 4 bits, appending tokens to it, decoding
+over it.
+
+A case names one operator and the sizes of its call; lengths follow from the
+case alone, tensor values from the seed alone. Keys, values and queries have the
+statistics of the workloads in paper_2607_29591_amd/synth.py. `run` computes a
+case in elementary torch operations, or, with `own` set, through the library.
+"""
+
+import math
+import random
+
+import torch
+
+own = False
+
+TAU, ALPHA, G_MIN, BETA = 0.25, 12.0, 0.0, 1.0
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+# ------------------------------------------------------------------- cases
+
+def _rope(name, dtype, B, Hq, Hkv, d, rows, rows_min, start, layout, rot, scaling, token_major, mix):
+    c = dict(kind="rope", dtype=dtype, B=B, Hq=Hq, Hkv=Hkv, d=d, rows=rows, rows_min=rows_min, start=start,
+             layout=layout, rot=rot, scaling=scaling, token_major=token_major, mix=mix)
+    return dict(c, name=name) if name else c
+
+
+def _cache(name, kind, dtype, B, Hq, Hkv, d, budget, budget_min, res_max, room, mix, rows=1, rows_min=1, rope=False,
+           layout="half", rot=0, scaling="none", append=False, tau=False):
+    c = dict(kind=kind, dtype=dtype, B=B, Hq=Hq, Hkv=Hkv, d=d, budget=budget, budget_min=budget_min, res_max=res_max,
+             room=room, rows=rows, rows_min=rows_min, rope=rope, layout=layout, rot=rot or d, scaling=scaling,
+             append=append, tau=tau, mix=mix)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one user's next token, one layer: 32 query and 8 key rows, where only latency counts
+        _rope("rope_token_b1", "bf16", 1, 32, 8, 128, 1, 1, 40000, "half", 128, "llama3", True, 1),
+        # one user's 32K-token prompt out of its projection (token-major) into the layout the constructions read
+        _rope("rope_prompt_32k", "bf16", 1, 32, 8, 128, 32768, 32768, 0, "half", 128, "llama3", True, 2),
+        # uneven follow-up chunks in fp32, neighbouring pairs, half of the head, a context stretched by YaRN
+        _rope("rope_chunks_f32", "f32", 16, 28, 4, 64, 509, 37, 60000, "interleaved", 32, "yarn", False, 3),
+        # one user's built cache of a layer into 4 bits, and its values back
+        _cache("pack_llama_b1", "pack", "bf16", 1, 32, 8, 128, 512, 512, 128, 128, 4),
+        # the same for a full serving batch
+        _cache("pack_batch_b32", "pack", "bf16", 32, 32, 8, 128, 2048, 2048, 512, 256, 5),
+        # a serving batch's next tokens into its caches, keys rotated on the way
+        _cache("append_token_b32", "append", "bf16", 32, 32, 8, 128, 2048, 2048, 512, 256, 6, rope=True,
+               scaling="llama3"),
+        # four users' follow-up questions, of uneven length
+        _cache("append_chunk_b4", "append", "bf16", 4, 32, 8, 128, 1024, 700, 256, 500, 7, rows=500, rows_min=60,
+               rope=True, scaling="llama3"),
+        # the smallest decode step: a toy layer in fp32
+        _cache("decode_toy_f32", "decode", "f32", 1, 8, 2, 64, 128, 128, 32, 0, 8),
+        # one user's chat: rotate, append and attend over 512-slot caches
+        _cache("decode_llama_b1", "decode", "bf16", 1, 32, 8, 128, 512, 512, 128, 128, 9, rope=True,
+               scaling="llama3", append=True),
+        # one very long cache: few heads, many slots each
+        _cache("decode_long_b1", "decode", "bf16", 1, 32, 8, 128, 65000, 65000, 4096, 0, 10),
+        # a full serving batch, per-query thresholds, queries rotated in the call
+        _cache("decode_batch_b32", "decode", "bf16", 32, 32, 8, 128, 2048, 2048, 512, 256, 11, rope=True,
+               scaling="llama3", tau=True),
+        # a batch of uneven budgets (28 query heads over 4 KV heads), tokens appended
+        _cache("decode_ragged_gqa7", "decode", "bf16", 64, 28, 4, 128, 1024, 256, 256, 128, 12, rope=True,
+               layout="interleaved", append=True),
+    ]
+
+
+def draw(rng):
+    def logint(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    kind = rng.choice(["rope", "rope", "pack", "append", "decode", "decode", "decode"])
+    dtype, d = rng.choice([("bf16", 128), ("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+    G, Hkv = rng.choice([1, 2, 4, 4, 7, 8, 16]), rng.choice([1, 2, 4, 8])
+    layout, scaling = rng.choice(["half", "interleaved"]), rng.choice(["none", "linear", "ntk", "llama3", "yarn"])
+    rot = rng.choice([d, d, d // 2, d // 4])
+    mix = rng.randrange(1 << 20)
+    e = 2 if dtype == "bf16" else 4
+    if kind == "rope":
+        B, rows = logint(1, 32), logint(1, 32768)
+        while B * rows * (G + 1) * Hkv * d * e > 32768 * 40 * 256:
+            B, rows = max(1, B // 2), max(1, rows // 2)
+        return _rope("", dtype, B, G * Hkv, Hkv, d, rows, rng.randint(max(1, rows // 4), rows), logint(1, 100000) - 1,
+                     layout, rot, scaling, rng.random() < 0.5, mix)
+    B, budget = logint(1, 64), logint(2, 4000) if kind != "decode" or rng.random() < 0.7 else logint(4000, 60000)
+    while B * Hkv * budget * d * (e if kind != "decode" else 2) > 256 * 2048 * 256:
+        if B > 1:
+            B //= 2
+        else:
+            budget //= 2
+    lo = rng.randint(max(2, budget // 4), budget) if budget > 8 and rng.random() < 0.5 else budget
+    res = int(lo * rng.uniform(0, 0.5))
+    rows = logint(1, 300) if kind == "append" else 1
+    rows_min = rng.randint(1, rows)
+    append = kind == "decode" and rng.random() < 0.5
+    room = rows + rng.randrange(64) if kind == "append" else rng.choice([1, 16, 100]) if append else rng.randrange(32)
+    return _cache("", kind, dtype, B, G * Hkv, Hkv, d, budget, lo, res, room, mix, rows=rows, rows_min=rows_min,
+                  rope=kind == "append" or (kind == "decode" and rng.random() < 0.5), layout=layout, rot=rot,
+                  scaling=scaling, append=append, tau=rng.random() < 0.5)
+
+
+def _lengths(case):
+    """Per sequence: tokens of the call; per (sequence, KV head): residual and main slots."""
+    r = random.Random(case["mix"])
+    B, H = case["B"], case["Hkv"]
+    rows = [r.randint(case["rows_min"], case["rows"]) for _ in range(B)]
+    if case["kind"] == "rope":
+        start = [r.randint(case["start"] // 2, case["start"]) for _ in range(B)]
+        return rows, start, None, None
+    start = [r.randint(case["budget"], 131072) for _ in range(B)]
+    budget = [r.randint(case["budget_min"], case["budget"]) for _ in range(B)]
+    res = [[r.choice([0, case["res_max"] // 4, case["res_max"] // 2, case["res_max"]]) for _ in range(H)]
+           for _ in range(B)]
+    res = [[min(x, b - 1) for x in row] for row, b in zip(res, budget)]
+    return rows, start, res, [[b - x for x in row] for row, b in zip(res, budget)]
+
+
+def _dt(case):
+    return torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _rope_args(case):
+    """Arguments of the rotation's plan: base, and the stretching of the context where there is one."""
+    more = {"none": {}, "linear": dict(factor=4.0), "ntk": dict(factor=4.0),
+            "llama3": dict(theta=500000.0, factor=8.0, original_len=8192, low_freq_factor=1.0, high_freq_factor=4.0),
+            "yarn": dict(factor=16.0, original_len=4096, beta_fast=32.0, beta_slow=1.0)}[case["scaling"]]
+    return dict(dict(theta=10000.0), rot_dim=case["rot"], layout=case["layout"], scaling=case["scaling"], **more)
+
+
+# ------------------------------------------------- elementary torch operations
+
+def _frequencies(case):
+    """Radians a position of each pair (64 bits), and the factor on the rotated pairs."""
+    a, rot = _rope_args(case), case["rot"]
+    i = torch.arange(rot // 2, dtype=torch.float64, device="cuda")
+    base = a["theta"]
+    if case["scaling"] == "ntk" and rot > 2:
+        base = base * a["factor"] ** (rot / (rot - 2.0))
+    f = base ** (-2.0 * i / rot)
+    if case["scaling"] == "linear":
+        f = f / a["factor"]
+    if case["scaling"] == "llama3":
+        wave = 2.0 * math.pi / f
+        lo, hi = a["low_freq_factor"], a["high_freq_factor"]
+        t = ((a["original_len"] / wave - lo) / (hi - lo)).clamp(0.0, 1.0)
+        f = f * ((1.0 - t) / a["factor"] + t)
+    if case["scaling"] == "yarn":
+        def at(beta):
+            return rot * math.log(a["original_len"] / (beta * 2.0 * math.pi)) / (2.0 * math.log(base))
+        lo, hi = max(math.floor(at(a["beta_fast"])), 0), min(math.ceil(at(a["beta_slow"])), rot - 1)
+        g = ((i - lo) / max(hi - lo, 0.001)).clamp(0.0, 1.0)
+        f = f / a["factor"] * g + f * (1.0 - g)
+        return f, 0.1 * math.log(a["factor"]) + 1.0
+    return f, 1.0
+
+
+def _turned(case, x, pos, wide=False):
+    """Rows x [B, H, T, d] rotated by positions pos [B, T], in 32 bits (64 where a border follows), unrounded."""
+    rot, w = case["rot"], torch.float64 if wide else torch.float32
+    f, scale = _frequencies(case)
+    angle = pos.double()[:, None, :, None] * f
+    c, s = (angle.cos() * scale).to(w), (angle.sin() * scale).to(w)
+    x = x.to(w)
+    if case["layout"] == "half":
+        a, b = x[..., :rot // 2], x[..., rot // 2:rot]
+        return torch.cat([a * c - b * s, a * s + b * c, x[..., rot:]], -1)
+    a, b = x[..., 0:rot:2], x[..., 1:rot:2]
+    return torch.cat([torch.stack([a * c - b * s, a * s + b * c], -1).flatten(-2), x[..., rot:]], -1)
+
+
+def _narrow(x, dt):
+    """64-bit x rounded once to dt: through 32 bits rounded to odd, so that the second rounding sees what was cut."""
+    f = x.to(torch.float32)
+    if dt == torch.float32:
+        return f
+    f = torch.where(f.double().abs() > x.abs(), torch.nextafter(f, torch.zeros_like(f)), f)
+    return (f.view(torch.int32) | (f.double() != x).to(torch.int32)).view(torch.float32).to(dt)
+
+
+def _pow2(e):
+    """2^e in 32 bits, from the exponent's bits (a power function may be off in the last place, which moves ties)."""
+    return ((e + 127) << 23).to(torch.int32).view(torch.float32)
+
+
+def _quantized(x):
+    """The values that rows x [..., d] stand for in 4 bits (32 bits, exact), and their codes and scale bytes."""
+    g = x.float().unflatten(-1, (-1, 32))
+    bits = g.abs().amax(-1).contiguous().view(torch.int32)
+    byte = ((bits >> 23) - 2 + ((bits & 0x7fffff) > 0x600000).to(torch.int32)).clamp(2, 252)
+    y = g.abs() * _pow2(127 - byte)[..., None]
+    code = ((y > 0.25).to(torch.uint8) + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5.0))
+    value = torch.tensor(E2M1, device=x.device)[code.int()] * _pow2(byte - 127)[..., None]
+    value = torch.where(torch.signbit(g), -value, value)
+    return value.flatten(-2), (code + 8 * torch.signbit(g)).flatten(-2), byte.to(torch.uint8)
+
+
+def _fields(case, cache):
+    """Views of a 4-bit cache [B*Hkv, blocks of 64 slots, bytes]: key codes, value codes, key scales, value scales."""
+    d = case["d"]
+    k, v, ks, vs = cache.split([32 * d, 32 * d, 2 * d, 2 * d], -1)
+    lead = cache.shape[:2]
+    return (k.reshape(*lead, 64, d // 2),                                                  # slot, byte
+            v.reshape(*lead, 16, 16, 4, d // 32).transpose(-3, -2).reshape(*lead, 64, d // 2),  # group piece slot byte
+            ks.reshape(*lead, 16, d // 32, 4).permute(0, 1, 4, 2, 3).reshape(*lead, 64, d // 32),
+            vs.reshape(*lead, 4, d // 32, 4, 4).permute(0, 1, 4, 2, 5, 3).reshape(*lead, 64, d // 32))
+
+
+def _values(case, cache):
+    """Keys and values [B, Hkv, C, d] that a 4-bit cache stands for, in 32 bits."""
+    half = torch.tensor(E2M1 + tuple(-x for x in E2M1), device=cache.device)
+    both = torch.stack([half.repeat(16), half.repeat_interleave(16)], -1)                  # byte -> its two values
+
+    def rows(code, scale):
+        x = both[code.int()].flatten(-2).unflatten(-1, (-1, 32))
+        x = x * _pow2(scale.to(torch.int32) - 127)[..., None]
+        return x.reshape(case["B"], case["Hkv"], -1, case["d"])[:, :, :_capacity(case)]
+
+    kq, vq, ks, vs = _fields(case, cache)
+    return rows(kq, ks), rows(vq, vs)
+
+
+def _capacity(case):
+    return case["budget"] + case["room"]
+
+
+def _attended(q, K, V, logc, r, n, tau):
+    """Shared-softmax decode of q [B, H, G, d] over rows [B, H, C, d], in their type."""
+    C, d = K.shape[-2:]
+    slot = torch.arange(C, device=q.device)
+    a = torch.matmul(q, K.transpose(-1, -2).contiguous()) / math.sqrt(d)
+    is_res = (slot < r[..., None])[:, :, None]
+    is_main = ((slot >= r[..., None]) & (slot < (r + n)[..., None]))[:, :, None]
+    bias = torch.full_like(K[..., 0], -math.inf)
+    R = min(C, logc.shape[-1])
+    bias[..., :R] = BETA * logc[..., :R]
+    main = a.masked_fill(~is_main, -math.inf)
+    top = main.amax(-1, keepdim=True)
+    p = torch.exp(main - top)
+    total = p.sum(-1, keepdim=True)
+    gate = torch.sigmoid((tau[..., None] - 1.0 / total) * ALPHA).clamp(min=G_MIN)
+    rest = (a + bias[:, :, None]).masked_fill(~is_res, -math.inf) + torch.log(gate)
+    high = torch.maximum(top, rest.amax(-1, keepdim=True))
+    e = p * torch.exp(top - high) + torch.exp(rest - high)
+    return torch.matmul(e, V) / e.sum(-1, keepdim=True)
+
+
+# ------------------------------------------------------------------ inputs
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, generator=g, device="cuda", dtype=torch.float32)
+
+
+def _bias(g, *lead, d):
+    """Key bias on four channels of each head."""
+    ch = torch.rand((*lead, d), generator=g, device="cuda").argsort(dim=-1)[..., :4]
+    return torch.zeros((*lead, d), device="cuda").scatter_(-1, ch, 3.0 * _randn(g, *lead, 4))
+
+
+def _positions(case, start):
+    """[B, rows] int32: consecutive positions from each sequence's start."""
+    at = torch.tensor(start, dtype=torch.int32, device="cuda")[:, None]
+    return (at + torch.arange(case["rows"], dtype=torch.int32, device="cuda")).contiguous()
+
+
+def prepare(case, seed):
+    g, dt = _gen(seed), _dt(case)
+    B, Hq, H, d, T = (case[x] for x in ("B", "Hq", "Hkv", "d", "rows"))
+    rows, start, res, main = _lengths(case)
+    st = dict(case=case, pos=_positions(case, start), n_tok=torch.tensor(rows, dtype=torch.int32, device="cuda"))
+    if case["kind"] == "rope":
+        # projections as a model makes them: token-major [B, T, H, d], or head-major
+        order = (B, T, -1, d) if case["token_major"] else (B, -1, T, d)
+        for name, heads in (("q", Hq), ("k", H)):
+            x = _randn(g, *[heads if y < 0 else y for y in order]).to(dt)
+            st[name] = x.transpose(1, 2) if case["token_major"] else x
+        return st
+    C = _capacity(case)
+    r, n = torch.tensor(res, device="cuda"), torch.tensor(main, device="cuda")
+    st.update(r=r, n=n, res_len=r.to(torch.int32).reshape(-1), main_len0=n.to(torch.int32).reshape(-1),
+              main_len=n.to(torch.int32).reshape(-1))
+    Rcap = max(1, int(r.max()))
+    bias = _bias(g, B, H, d=d)[:, :, None]
+    # residual slots are means of `count` tokens: noise shrinks with the count, a few are empty
+    count = torch.exp(4.0 + _randn(g, B, H, Rcap)).floor() + 1.0
+    slot = torch.arange(C, device="cuda")
+    empty = torch.rand((B, H, Rcap), generator=g, device="cuda") < 0.02
+    is_res = (slot < r[..., None])[..., :Rcap]
+    st["logc"] = torch.where(is_res & ~empty, torch.log(count), torch.tensor(-math.inf, device="cuda"))
+    shrink = torch.ones((B, H, C), device="cuda")
+    shrink[..., :Rcap] = torch.where(is_res, count.rsqrt(), shrink[..., :Rcap])
+    K = _randn(g, B, H, C, d) * shrink[..., None] + bias
+    V = _randn(g, B, H, C, d) * shrink[..., None]
+    nh = max(4, case["budget"] // 32)
+    at = r[..., None] + (torch.rand((B, H, nh), generator=g, device="cuda") * n[..., None]).long()
+    at = at[..., None].expand(B, H, nh, d)
+    heavy = 3.0 * K.gather(2, at)
+    K.scatter_(2, at, heavy)
+    if case["kind"] == "pack":
+        st.update(kc=K.to(dt), vc=V.to(dt))
+        return st
+    st["cache"] = _laid_out(case, K, V)
+    del K, V
+    st["k_new"] = (_randn(g, B, H, T, d) + bias).to(dt)
+    st["v_new"] = _randn(g, B, H, T, d).to(dt)
+    if case["kind"] == "decode":
+        G = Hq // H
+        pick = torch.randint(nh, (B, H, G * 4), generator=g, device="cuda")
+        q = torch.gather(heavy, 2, pick[..., None].expand(B, H, G * 4, d)).reshape(B, H, G, 4, d).mean(3)
+        q = (0.7 * q + 0.3 * _randn(g, B, H, G, d)).reshape(B, Hq, d)
+        if case["rope"]:   # turned back, so that the rotated queries meet the heavy keys
+            q = _turned(case, q[:, :, None], -st["pos"])[:, :, 0] / _frequencies(case)[1] ** 2
+        st["q"] = q.to(dt).contiguous()
+        st["tau"] = 0.5 * _randn(g, B, Hq) if case["tau"] else None
+    return st
+
+
+def _laid_out(case, K, V):
+    """Rows [B, Hkv, C, d] as a 4-bit cache [B*Hkv, blocks of 64 slots, bytes]; slots past C zero."""
+    B, H, C, d = K.shape
+    nb = -(-C // 64)
+
+    def parts(x):
+        _, code, byte = _quantized(torch.nn.functional.pad(x, (0, 0, 0, 64 * nb - C)).reshape(B * H, nb, 64, d))
+        return code[..., 0::2] + 16 * code[..., 1::2], byte
+
+    (kq, ks), (vq, vs) = parts(K), parts(V)
+    vq = vq.reshape(B * H, nb, 16, 4, 16, d // 32).transpose(-3, -2)
+    ks = ks.reshape(B * H, nb, 4, 16, d // 32).permute(0, 1, 3, 4, 2)
+    vs = vs.reshape(B * H, nb, 4, 4, 4, d // 32).permute(0, 1, 3, 5, 2, 4)
+    return torch.cat([x.reshape(B * H, nb, -1) for x in (kq, vq, ks, vs)], -1).contiguous()
+
+
+# --------------------------------------------------------------------- run
+
+def run(st):
+    return _run_own(st) if own else _run_plain(st)
+
+
+def _run_plain(st):
+    case, dt = st["case"], _dt(st["case"])
+    kind, T = case["kind"], case["rows"]
+    live = (torch.arange(T, device="cuda") < st["n_tok"][:, None])[:, None, :, None]
+    if kind == "rope":
+        return {x: torch.where(live, _turned(case, st[x], st["pos"]), 0.0).to(dt) for x in ("q", "k")}
+    C, end = _capacity(case), (st["r"] + st["n"])[..., None]
+    if kind == "pack":
+        used = (torch.arange(C, device="cuda") < end)[..., None]
+        return {x: torch.where(used, _quantized(st[x])[0], 0.0).to(dt) for x in ("kc", "vc")}
+    k, v = st["k_new"], st["v_new"]
+    if case["rope"]:
+        k = _narrow(_turned(case, k, st["pos"], wide=True), dt)
+    k, v = _quantized(k)[0], _quantized(v)[0]
+    if kind == "append":
+        return {"k": torch.where(live, k, 0.0).to(dt), "v": torch.where(live, v, 0.0).to(dt),
+                "main_len": st["main_len0"] + st["n_tok"].repeat_interleave(case["Hkv"])}
+    K, V = _values(case, st["cache"])
+    n, got = st["n"], {}
+    if case["append"]:
+        at = end[..., None].expand(*k.shape)
+        K, V, n = K.scatter(2, at, k), V.scatter(2, at, v), n + 1
+        got = {"k": k.to(dt), "v": v.to(dt), "main_len": st["main_len0"] + 1}
+    q = st["q"]
+    if case["rope"]:
+        q = _narrow(_turned(case, q[:, :, None], st["pos"], wide=True)[:, :, 0], dt)
+    B, H, d = case["B"], case["Hkv"], case["d"]
+    tau = torch.full((B, case["Hq"]), TAU, device="cuda") if st["tau"] is None else st["tau"]
+    o = _attended(q.float().reshape(B, H, -1, d), K, V, st["logc"], st["r"], n, tau.reshape(B, H, -1))
+    return dict(got, out=o.reshape(B, -1, d))
+
+
+def _handles(st):
+    """What a program makes once and keeps: the shape, the rotation's plan, output buffers, workspace."""
+    from paper_2607_29591_amd import reskv as rk
+    case, dt = st["case"], _dt(st["case"])
+    B, Hq, H, d, T, kind = (case[x] for x in ("B", "Hq", "Hkv", "d", "rows", "kind"))
+    rope = rk.make_rope(**_rope_args(case)) if case.get("rope", True) else None
+
+    def zeros(*shape):
+        return torch.zeros(shape, dtype=dt, device="cuda")
+    if kind == "rope":
+        return dict(rk=rk, shape=rk.make_shape(B, Hq, H, d, case["dtype"], 1, 1), rope=rope,
+                    q_out=zeros(B, Hq, T, d), k_out=zeros(B, H, T, d))
+    C = _capacity(case)
+    h = dict(rk=rk, shape=rk.make_shape(B, Hq, H, d, case["dtype"], C, st["logc"].shape[-1]), rope=rope,
+             first=(st["res_len"] + st["main_len0"]).contiguous())
+    if kind == "pack":
+        return dict(h, cache=torch.zeros(rk.reskv_q4_cache_size(h["shape"]), dtype=torch.uint8, device="cuda"),
+                    k=zeros(B, H, C, d), v=zeros(B, H, C, d))
+    h.update(k=zeros(B, H, T, d), v=zeros(B, H, T, d))
+    if kind == "decode":
+        gate = rk.make_gate(tau=st["tau"], tau_scalar=TAU, alpha=ALPHA, g_min=G_MIN, beta=BETA)
+        h["out"] = torch.zeros((B, Hq, d), dtype=torch.float32, device="cuda")
+        h["ws"] = torch.empty(rk.reskv_decode_q4_workspace_size(h["shape"]), dtype=torch.uint8, device="cuda")
+        new = dict(k_new=st["k_new"][:, :, 0], v_new=st["v_new"][:, :, 0]) if case["append"] else {}
+        turn = dict(rope=rope, positions=st["pos"]) if case["rope"] else {}
+        h["call"] = rk.prepare_decode_attn_q4(h["shape"], gate, st["q"], st["cache"], st["logc"], st["res_len"],
+                                              st["main_len"], h["out"], h["ws"], **turn, **new)
+    return h
+
+
+def _run_own(st):
+    if "handles" not in st:
+        st["handles"] = _handles(st)
+    case, h = st["case"], st["handles"]
+    rk, kind = h["rk"], case["kind"]
+    if kind == "rope":
+        rk.reskv_rope(h["shape"], h["rope"], st["pos"], q=st["q"], q_out=h["q_out"], k=st["k"], k_out=h["k_out"],
+                      n_tok=st["n_tok"])
+        return {"q": h["q_out"], "k": h["k_out"]}
+    if kind == "pack":
+        rk.reskv_pack_q4(h["shape"], st["kc"], st["vc"], st["res_len"], st["main_len"], h["cache"])
+        rk.reskv_unpack_q4(h["shape"], h["cache"], st["res_len"], st["main_len"], h["k"], h["v"])
+        return {"kc": h["k"], "vc": h["v"]}
+    if kind == "append" or case["append"]:
+        st["main_len"].copy_(st["main_len0"])   # the pass appends the same tokens again
+    if kind == "append":
+        rk.reskv_append_kv_q4(h["shape"], st["k_new"], st["v_new"], st["cache"], st["res_len"], st["main_len"],
+                              rope=h["rope"], positions=st["pos"], n_tok=st["n_tok"])
+    else:
+        h["call"]()
+    got = {} if kind == "append" else {"out": h["out"]}
+    if kind == "append" or case["append"]:   # the rows that were appended, read back from the cache
+        rk.reskv_unpack_q4(h["shape"], st["cache"], st["res_len"], st["main_len"], h["k"], h["v"],
+                           first_slot=h["first"])
+        got.update(k=h["k"], v=h["v"], main_len=st["main_len"])
+    return got
+
+
+# -------------------------------------------------------------------- work
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    B, Hq, H, d = (case[x] for x in ("B", "Hq", "Hkv", "d"))
+    rows, _, res, main = _lengths(case)
+    if case["kind"] == "rope":
+        n = sum(rows) * (Hq + H)
+        return {"bytes": 2 * n * d * e + 4 * sum(rows), "flops": 3 * n * case["rot"]}
+    slot = 2 * (d // 2 + d // 32)    # 4-bit keys and values of a slot with their scales
+    live = sum(map(sum, res)) + sum(map(sum, main))
+    if case["kind"] == "pack":       # rows read, the cache written, its values written
+        return {"bytes": live * (4 * d * e + slot), "flops": 2 * live * 2 * d}
+    if case["kind"] == "append":     # tokens read, their slots written, their values written
+        n = sum(rows) * H
+        return {"bytes": n * (4 * d * e + slot) + 12 * B * H, "flops": n * (3 * case["rot"] + 4 * d)}
+    new = B * H if case["append"] else 0
+    nbytes = live * slot + 4 * sum(map(sum, res)) + B * Hq * d * (e + 4) + 8 * B * H + new * (4 * d * e + slot)
+    return {"bytes": nbytes, "flops": 4 * (Hq // H) * d * (live + new)}
+
+
+# --------------------------------------------- 64-bit values from the definitions
+
+def _turned64(case, x, pos):
+    """Rows x rotated as complex numbers, x [B, H, T, d] and pos [B, T]."""
+    a, rot = _rope_args(case), case["rot"]
+    s, theta, freq, scale = a.get("factor", 1.0), a["theta"], [], 1.0
+    if case["scaling"] == "yarn":
+        scale = 1.0 + math.log(s) / 10.0
+        turns = [a["original_len"] / (2.0 * math.pi * b) for b in (a["beta_fast"], a["beta_slow"])]
+        first, last = (rot / 2.0 * math.log(t) / math.log(theta) for t in turns)
+        first, last = max(0, math.floor(first)), min(rot - 1, math.ceil(last))
+    for i in range(rot // 2):
+        f = math.pow(theta, -2.0 * i / rot)
+        if case["scaling"] == "linear":
+            f /= s
+        elif case["scaling"] == "ntk":
+            f = math.pow(theta * math.pow(s, rot / (rot - 2.0)), -2.0 * i / rot) if rot > 2 else f
+        elif case["scaling"] == "llama3":
+            turn = a["original_len"] * f / (2.0 * math.pi)        # rotations over the original context
+            if turn < a["low_freq_factor"]:
+                f /= s
+            elif turn <= a["high_freq_factor"]:
+                t = (turn - a["low_freq_factor"]) / (a["high_freq_factor"] - a["low_freq_factor"])
+                f = (1.0 - t) * f / s + t * f
+        elif case["scaling"] == "yarn":
+            t = min(1.0, max(0.0, (i - first) / max(0.001, last - first)))
+            f = t * (f / s) + (1.0 - t) * f
+        freq.append(f)
+    angle = pos.double()[:, None, :, None] * torch.tensor(freq, dtype=torch.float64, device=x.device)
+    turn = torch.polar(torch.full_like(angle, scale), angle)
+    x = x.double()
+    if case["layout"] == "half":
+        z = torch.complex(x[..., :rot // 2].contiguous(), x[..., rot // 2:rot].contiguous()) * turn
+        return torch.cat([z.real, z.imag, x[..., rot:]], -1)
+    z = torch.view_as_complex(x[..., :rot].unflatten(-1, (-1, 2)).contiguous()) * turn
+    return torch.cat([torch.view_as_real(z).flatten(-2), x[..., rot:]], -1)
+
+
+def _times2(x, e):
+    """x * 2^e for whole e, exactly."""
+    return x * ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _stored64(x, dt):
+    """x as the type dt holds it: the nearest number of 8 or 24 significant digits, ties to even."""
+    digits = 8 if dt == torch.bfloat16 else 24
+    m, ex = torch.frexp(x)
+    return _times2(torch.round(m * 2.0 ** digits), ex - digits)
+
+
+def _quantized64(x):
+    """Nearest of the fifteen 4-bit values at each block's scale, ties to the even code."""
+    g = x.double().unflatten(-1, (-1, 32))
+    top = g.abs().amax(-1, keepdim=True)
+    # the least power of two under which no value passes 7, where clipping to 6 costs half a step
+    e = torch.where(top > 0, torch.ceil(torch.log2(top / 7.0)), torch.tensor(-125.0, dtype=top.dtype, device=x.device))
+    e = torch.where(_times2(top, -e) > 7.0, e + 1, torch.where(_times2(top, -e) <= 3.5, e - 1, e)).clamp(-125, 125)
+    y = _times2(g, -e)
+    a = y.abs()
+    step = torch.where(a < 2.0, 0.5, torch.where(a < 4.0, 1.0, 2.0))
+    return _times2(torch.copysign(torch.clamp(torch.round(a / step) * step, max=6.0), y), e).flatten(-2)
+
+
+def _values64(case, cache):
+    """Keys and values of a 4-bit cache, slot by slot from the layout's definition."""
+    d, C = case["d"], _capacity(case)
+    slot, i = torch.arange(C, device=cache.device)[:, None], torch.arange(d, device=cache.device)[None]
+    base, s = (slot // 64) * (68 * d), slot % 64
+    flat, piece = cache.reshape(cache.shape[0], -1), d // 16
+    kb = base + s * (d // 2) + i // 2
+    vb = base + 32 * d + ((s // 4) * 16 + i // piece) * 2 * piece + (s % 4) * (piece // 2) + (i % piece) // 2
+    ksc = base + 64 * d + ((s % 16) * (d // 32) + i // 32) * 4 + s // 16
+    vsc = base + 66 * d + ((((s // 4) % 4) * (d // 32) + i // 32) * 4 + s // 16) * 4 + s % 4
+
+    def read(code, scale):
+        c = (flat[:, code].int() >> (4 * (i % 2)).int()) & 15
+        e, m = (c >> 1) & 3, (c & 1).double()
+        x = torch.where(e == 0, 0.5 * m, _times2(1.0 + 0.5 * m, e - 1)) * (1.0 - 2.0 * (c >> 3))
+        return _times2(x, flat[:, scale].int() - 127).reshape(case["B"], case["Hkv"], C, d)
+
+    return read(kb, ksc), read(vb, vsc)
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    B, Hq, H, d, T, kind = (case[x] for x in ("B", "Hq", "Hkv", "d", "rows", "kind"))
+    rows, start, res, main = _lengths(case)
+    pos = torch.tensor([[s + t for t in range(T)] for s in start], device="cuda")
+    pad = torch.tensor([[t >= n for t in range(T)] for n in rows], device="cuda")[:, None, :, None]
+    if kind == "rope":
+        return {x: _turned64(case, st[x], pos).masked_fill(pad, 0.0) for x in ("q", "k")}
+    r, n = torch.tensor(res, device="cuda"), torch.tensor(main, device="cuda")
+    C = _capacity(case)
+    if kind == "pack":
+        dead = (torch.arange(C, device="cuda") >= (r + n)[..., None])[..., None]
+        return {x: _quantized64(st[x]).masked_fill(dead, 0.0) for x in ("kc", "vc")}
+
+    def stored(x):
+        return _stored64(_turned64(case, x, pos), _dt(case)) if case["rope"] else x.double()
+
+    k, v = _quantized64(stored(st["k_new"])), _quantized64(st["v_new"])
+    if kind == "append":
+        return {"k": k.masked_fill(pad, 0.0), "v": v.masked_fill(pad, 0.0),
+                "main_len": torch.tensor([m + t for row, t in zip(main, rows) for m in row], dtype=torch.int32)}
+    K, V = _values64(case, st["cache"])
+    got = {}
+    if case["append"]:
+        b, h = torch.meshgrid(torch.arange(B, device="cuda"), torch.arange(H, device="cuda"), indexing="ij")
+        K[b, h, r + n], V[b, h, r + n] = k[:, :, 0], v[:, :, 0]
+        n = n + 1
+        got = {"k": k, "v": v, "main_len": n.to(torch.int32).reshape(-1)}
+    q = stored(st["q"][:, :, None]).reshape(B, H, Hq // H, d)
+    tau = torch.full((B, H, Hq // H), TAU, dtype=torch.float64, device="cuda")
+    if st["tau"] is not None:
+        tau = st["tau"].double().reshape(B, H, -1)
+    out = []
+    for b in range(B):          # branch by branch under its own softmax, joined by log-sum-exps
+        slot = torch.arange(C, device="cuda")
+        a = torch.matmul(q[b], K[b].transpose(-1, -2).contiguous()) / math.sqrt(d)
+        am = a.masked_fill(((slot < r[b][:, None]) | (slot >= (r + n)[b][:, None]))[:, None], -math.inf)
+        c = torch.nn.functional.pad(st["logc"][b].double(), (0, C))[:, :C]
+        ar = (a + BETA * c[:, None]).masked_fill((slot >= r[b][:, None])[:, None], -math.inf)
+        lm, lr = torch.logsumexp(am, -1), torch.logsumexp(ar, -1)
+        gate = torch.sigmoid(ALPHA * (tau[b] - torch.exp(am.amax(-1) - lm))).clamp(min=G_MIN)
+        om = torch.matmul(torch.softmax(am, -1), V[b])
+        has = torch.isfinite(lr)
+        orr = torch.matmul(torch.softmax(torch.where(has[..., None], ar, 0.0), -1), V[b])
+        share = torch.where(has, torch.sigmoid(torch.where(has, lr, 0.0) + torch.log(gate) - lm), 0.0)[..., None]
+        out.append(om + (orr - om) * share)
+    return dict(got, out=torch.stack(out).reshape(B, Hq, d))
