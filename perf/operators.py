@@ -394,16 +394,16 @@ def _handles(st):
     h = dict(rk=rk, shape=rk.make_shape(B, Hq, H, d, case["dtype"], C, st["logc"].shape[-1]), rope=rope,
              first=(st["res_len"] + st["main_len0"]).contiguous())
     if kind == "pack":
-        return dict(h, cache=torch.zeros(rk.reskv_q4_cache_size(h["shape"]), dtype=torch.uint8, device="cuda"),
+        return dict(h, cache=torch.zeros(rk.reskv_quant_cache_size(h["shape"]), dtype=torch.uint8, device="cuda"),
                     k=zeros(B, H, C, d), v=zeros(B, H, C, d))
     h.update(k=zeros(B, H, T, d), v=zeros(B, H, T, d))
     if kind == "decode":
         gate = rk.make_gate(tau=st["tau"], tau_scalar=TAU, alpha=ALPHA, g_min=G_MIN, beta=BETA)
         h["out"] = torch.zeros((B, Hq, d), dtype=torch.float32, device="cuda")
-        h["ws"] = torch.empty(rk.reskv_decode_q4_workspace_size(h["shape"]), dtype=torch.uint8, device="cuda")
+        h["ws"] = torch.empty(rk.reskv_decode_quant_workspace_size(h["shape"]), dtype=torch.uint8, device="cuda")
         new = dict(k_new=st["k_new"][:, :, 0], v_new=st["v_new"][:, :, 0]) if case["append"] else {}
         turn = dict(rope=rope, positions=st["pos"]) if case["rope"] else {}
-        h["call"] = rk.prepare_decode_attn_q4(h["shape"], gate, st["q"], st["cache"], st["logc"], st["res_len"],
+        h["call"] = rk.prepare_decode_attn_quant(h["shape"], gate, st["q"], st["cache"], st["logc"], st["res_len"],
                                               st["main_len"], h["out"], h["ws"], **turn, **new)
     return h
 
@@ -418,19 +418,19 @@ def _run_own(st):
                       n_tok=st["n_tok"])
         return {"q": h["q_out"], "k": h["k_out"]}
     if kind == "pack":
-        rk.reskv_pack_q4(h["shape"], st["kc"], st["vc"], st["res_len"], st["main_len"], h["cache"])
-        rk.reskv_unpack_q4(h["shape"], h["cache"], st["res_len"], st["main_len"], h["k"], h["v"])
+        rk.reskv_pack_quant(h["shape"], st["kc"], st["vc"], st["res_len"], st["main_len"], h["cache"])
+        rk.reskv_unpack_quant(h["shape"], h["cache"], st["res_len"], st["main_len"], h["k"], h["v"])
         return {"kc": h["k"], "vc": h["v"]}
     if kind == "append" or case["append"]:
         st["main_len"].copy_(st["main_len0"])   # the pass appends the same tokens again
     if kind == "append":
-        rk.reskv_append_kv_q4(h["shape"], st["k_new"], st["v_new"], st["cache"], st["res_len"], st["main_len"],
+        rk.reskv_append_kv_quant(h["shape"], st["k_new"], st["v_new"], st["cache"], st["res_len"], st["main_len"],
                               rope=h["rope"], positions=st["pos"], n_tok=st["n_tok"])
     else:
         h["call"]()
     got = {} if kind == "append" else {"out": h["out"]}
     if kind == "append" or case["append"]:   # the rows that were appended, read back from the cache
-        rk.reskv_unpack_q4(h["shape"], st["cache"], st["res_len"], st["main_len"], h["k"], h["v"],
+        rk.reskv_unpack_quant(h["shape"], st["cache"], st["res_len"], st["main_len"], h["k"], h["v"],
                            first_slot=h["first"])
         got.update(k=h["k"], v=h["v"], main_len=st["main_len"])
     return got
