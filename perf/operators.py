@@ -379,7 +379,8 @@ def _run_plain(st):
 
 
 def _handles(st):
-    """What a program makes once and keeps: the shape, the rotation's plan, output buffers, workspace."""
+    """What a program makes once and keeps: the shape, the rotation's plan, output buffers, the workspace, and its
+    calls with their arguments marshalled, as a serving loop keeps them."""
     from paper_2607_29591_amd import reskv as rk
     case, dt = st["case"], _dt(st["case"])
     B, Hq, H, d, T, kind = (case[x] for x in ("B", "Hq", "Hkv", "d", "rows", "kind"))
@@ -388,23 +389,32 @@ def _handles(st):
     def zeros(*shape):
         return torch.zeros(shape, dtype=dt, device="cuda")
     if kind == "rope":
-        return dict(rk=rk, shape=rk.make_shape(B, Hq, H, d, case["dtype"], 1, 1), rope=rope,
-                    q_out=zeros(B, Hq, T, d), k_out=zeros(B, H, T, d))
+        h = dict(q=zeros(B, Hq, T, d), k=zeros(B, H, T, d))
+        call = rk.prepare_rope(rk.make_shape(B, Hq, H, d, case["dtype"], 1, 1), rope, st["pos"], q=st["q"],
+                               q_out=h["q"], k=st["k"], k_out=h["k"], n_tok=st["n_tok"])
+        return dict(h, calls=[call])
     C = _capacity(case)
-    h = dict(rk=rk, shape=rk.make_shape(B, Hq, H, d, case["dtype"], C, st["logc"].shape[-1]), rope=rope,
-             first=(st["res_len"] + st["main_len0"]).contiguous())
+    shape = rk.make_shape(B, Hq, H, d, case["dtype"], C, st["logc"].shape[-1])
+    lens = (st["res_len"], st["main_len"])
     if kind == "pack":
-        return dict(h, cache=torch.zeros(rk.reskv_quant_cache_size(h["shape"]), dtype=torch.uint8, device="cuda"),
-                    k=zeros(B, H, C, d), v=zeros(B, H, C, d))
-    h.update(k=zeros(B, H, T, d), v=zeros(B, H, T, d))
-    if kind == "decode":
+        h = dict(cache=torch.zeros(rk.reskv_quant_cache_size(shape), dtype=torch.uint8, device="cuda"),
+                 k=zeros(B, H, C, d), v=zeros(B, H, C, d))
+        return dict(h, calls=[rk.prepare_pack_quant(shape, st["kc"], st["vc"], *lens, h["cache"]),
+                              rk.prepare_unpack_quant(shape, h["cache"], *lens, h["k"], h["v"])])
+    h = dict(k=zeros(B, H, T, d), v=zeros(B, H, T, d), first=(st["res_len"] + st["main_len0"]).contiguous(), calls=[])
+    turn = dict(rope=rope, positions=st["pos"]) if case["rope"] else {}
+    if kind == "append":
+        h["calls"].append(rk.prepare_append_kv_quant(shape, st["k_new"], st["v_new"], st["cache"], *lens,
+                                                     n_tok=st["n_tok"], **turn))
+    else:
         gate = rk.make_gate(tau=st["tau"], tau_scalar=TAU, alpha=ALPHA, g_min=G_MIN, beta=BETA)
         h["out"] = torch.zeros((B, Hq, d), dtype=torch.float32, device="cuda")
-        h["ws"] = torch.empty(rk.reskv_decode_quant_workspace_size(h["shape"]), dtype=torch.uint8, device="cuda")
+        h["ws"] = torch.empty(rk.reskv_decode_quant_workspace_size(shape), dtype=torch.uint8, device="cuda")
         new = dict(k_new=st["k_new"][:, :, 0], v_new=st["v_new"][:, :, 0]) if case["append"] else {}
-        turn = dict(rope=rope, positions=st["pos"]) if case["rope"] else {}
-        h["call"] = rk.prepare_decode_attn_quant(h["shape"], gate, st["q"], st["cache"], st["logc"], st["res_len"],
-                                              st["main_len"], h["out"], h["ws"], **turn, **new)
+        h["calls"].append(rk.prepare_decode_attn_quant(shape, gate, st["q"], st["cache"], st["logc"], *lens, h["out"],
+                                                       h["ws"], **turn, **new))
+    if kind == "append" or case["append"]:   # the rows that were appended, read back from the cache
+        h["calls"].append(rk.prepare_unpack_quant(shape, st["cache"], *lens, h["k"], h["v"], first_slot=h["first"]))
     return h
 
 
@@ -412,26 +422,16 @@ def _run_own(st):
     if "handles" not in st:
         st["handles"] = _handles(st)
     case, h = st["case"], st["handles"]
-    rk, kind = h["rk"], case["kind"]
-    if kind == "rope":
-        rk.reskv_rope(h["shape"], h["rope"], st["pos"], q=st["q"], q_out=h["q_out"], k=st["k"], k_out=h["k_out"],
-                      n_tok=st["n_tok"])
-        return {"q": h["q_out"], "k": h["k_out"]}
-    if kind == "pack":
-        rk.reskv_pack_quant(h["shape"], st["kc"], st["vc"], st["res_len"], st["main_len"], h["cache"])
-        rk.reskv_unpack_quant(h["shape"], h["cache"], st["res_len"], st["main_len"], h["k"], h["v"])
-        return {"kc": h["k"], "vc": h["v"]}
-    if kind == "append" or case["append"]:
+    if case["kind"] == "append" or case.get("append"):
         st["main_len"].copy_(st["main_len0"])   # the pass appends the same tokens again
-    if kind == "append":
-        rk.reskv_append_kv_quant(h["shape"], st["k_new"], st["v_new"], st["cache"], st["res_len"], st["main_len"],
-                              rope=h["rope"], positions=st["pos"], n_tok=st["n_tok"])
-    else:
-        h["call"]()
-    got = {} if kind == "append" else {"out": h["out"]}
-    if kind == "append" or case["append"]:   # the rows that were appended, read back from the cache
-        rk.reskv_unpack_quant(h["shape"], st["cache"], st["res_len"], st["main_len"], h["k"], h["v"],
-                           first_slot=h["first"])
+    for call in h["calls"]:
+        call()
+    if case["kind"] == "rope":
+        return {"q": h["q"], "k": h["k"]}
+    if case["kind"] == "pack":
+        return {"kc": h["k"], "vc": h["v"]}
+    got = {"out": h["out"]} if case["kind"] == "decode" else {}
+    if case["kind"] == "append" or case["append"]:
         got.update(k=h["k"], v=h["v"], main_len=st["main_len"])
     return got
 
