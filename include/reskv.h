@@ -487,6 +487,187 @@ reskv_status_t reskv_append_kv(const reskv_shape_t* shape,
                                const int32_t* res_len, int32_t* main_len,
                                void* stream);
 
+/*
+ * ---- Rotary positions ------------------------------------------------------
+ *
+ * A rotation plan holds, for each of the rot_dim / 2 pairs of a row, the
+ * radians a position turns it by. With f_i = theta^(-2 i / rot_dim):
+ *   NONE     f_i
+ *   LINEAR   f_i / factor
+ *   NTK      f_i at the base theta * factor^(rot_dim / (rot_dim - 2))
+ *   LLAMA3   with n_i = original_len * f_i / (2 pi) turns over the original
+ *            context: f_i / factor where n_i < low_freq_factor, f_i where
+ *            n_i > high_freq_factor, between them ((1 - t) / factor + t) f_i,
+ *            t = (n_i - low) / (high - low)
+ *   YARN     ((1 - t) + t / factor) f_i with t = (i - lo) / (hi - lo) clamped
+ *            to [0, 1] (hi - lo at least 0.001), lo = max(floor(dim(beta_fast)),
+ *            0), hi = min(ceil(dim(beta_slow)), rot_dim - 1), dim(n) = rot_dim *
+ *            ln(original_len / (2 pi n)) / (2 ln theta); rotated pairs are also
+ *            multiplied by 0.1 ln(factor) + 1 unless attn_scale is given
+ * The pair i of a row is (x_i, x_{i + rot_dim/2}) in the HALF layout and
+ * (x_{2i}, x_{2i+1}) in the INTERLEAVED one; at position p it becomes
+ *   (A (x cos a - y sin a), A (x sin a + y cos a)),  a = p f_i,  A = attn_scale;
+ * elements from rot_dim on stay as they are. Angles, sines and products are
+ * computed in 64 bits and every result is rounded once to the row's type.
+ */
+typedef enum { RESKV_ROPE_HALF = 0, RESKV_ROPE_INTERLEAVED = 1 } reskv_rope_layout_t;
+typedef enum {
+  RESKV_ROPE_NONE = 0,
+  RESKV_ROPE_LINEAR = 1,
+  RESKV_ROPE_NTK = 2,
+  RESKV_ROPE_LLAMA3 = 3,
+  RESKV_ROPE_YARN = 4
+} reskv_rope_scaling_t;
+
+typedef struct {
+  int32_t rot_dim;      /* rotated elements of a row: a multiple of 16, 16..128 */
+  int32_t layout;       /* reskv_rope_layout_t */
+  int32_t scaling;      /* reskv_rope_scaling_t */
+  double theta;         /* base, > 1 (10000 in most models) */
+  double factor;        /* context stretching, >= 1 (all but NONE) */
+  double original_len;  /* context before stretching, > 0 (LLAMA3, YARN) */
+  double low_freq_factor, high_freq_factor;  /* 0 < low < high (LLAMA3) */
+  double beta_fast, beta_slow;               /* beta_fast > beta_slow > 0 (YARN) */
+  double attn_scale;    /* A; 0 takes the scaling's own (1, but for YARN) */
+} reskv_rope_params_t;
+
+typedef struct {        /* a plan, filled by reskv_rope_init; plain data */
+  int32_t rot_dim, layout;
+  double attn_scale;
+  double freq[64];      /* radians a position, pairs [0, rot_dim / 2) */
+} reskv_rope_t;
+
+/* Fill a rotation plan (host only; no GPU work). */
+reskv_status_t reskv_rope_init(const reskv_rope_params_t* params, reskv_rope_t* rope);
+
+typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
+  int64_t batch, head, row;  /* strides in elements; elements of a row adjoin */
+} reskv_rows_t;
+
+/*
+ * reskv_rope - rotate the rows of queries and keys by their positions.
+ *
+ *   shape           batch, num_q_heads, num_kv_heads, head_dim, dtype
+ *                   (slot_cap and res_cap are not used)
+ *   rope            plan; rot_dim <= head_dim
+ *   n_rows          rows n per sequence and head, >= 0 (a decode step has 1)
+ *   positions       [B, n] int32, device; negative positions turn back
+ *   n_tok           [B] int32, device, or NULL: rows t >= n_tok[b] are padding,
+ *                   their outputs are left as they were
+ *   q, q_at         [B, Hq, n, d] by strides, or NULL: keys only
+ *   q_out, q_out_at where the rotated queries go
+ *   k, k_at, k_out, k_out_at   the same for keys [B, Hkv, n, d], or NULL
+ *
+ * Any order of heads and rows is taken (a projection's [B, n, heads, d], a part
+ * of a fused one), so the call also moves rows into the layout that the
+ * constructions read. An output may be its input (the same pointer and
+ * strides); otherwise an output overlaps no input, and its rows do not overlap
+ * each other. Pointers are aligned to 16 bytes, strides are multiples of 16 bytes.
+ */
+reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope,
+                          int32_t n_rows, const int32_t* positions, const int32_t* n_tok,
+                          const void* q, const reskv_rows_t* q_at,
+                          void* q_out, const reskv_rows_t* q_out_at,
+                          const void* k, const reskv_rows_t* k_at,
+                          void* k_out, const reskv_rows_t* k_out_at,
+                          void* stream);
+
+/*
+ * ---- Caches in 4 bits ------------------------------------------------------
+ *
+ * A built cache (kc, vc of the constructions) held in 4 bits a number: along a
+ * row, every 32 elements share a power-of-two scale 2^(e - 127), e one byte,
+ * and each element is one of 0, .5, 1, 1.5, 2, 3, 4, 6 with a sign (codes 0..7
+ * in that order, 8 added for the sign) times that scale. e is the least for
+ * which no magnitude passes 7 scales (above 6, clipping costs at most half a
+ * step), within [2, 252]; elements are rounded to the nearest value, ties to
+ * the even code, magnitudes above 6 scales to 6. A group with a NaN or an
+ * infinity gets e = 255: all its elements stand for NaN. logc, main_idx,
+ * res_len and main_len stay as the constructions write them.
+ *
+ * Layout of the buffer: per (b, kv head) ceil(C / 64) blocks of 68 d bytes, one
+ * for 64 slots; in a block, for slot s and element i (P = d / 16), the low
+ * nibble of a byte for even i, the high one for odd i:
+ *   key codes    at 0:     s d/2 + i/2
+ *   value codes  at 32 d:  ((s/4) 16 + i/P) 2P + (s%4) P/2 + (i%P)/2
+ *   key scales   at 64 d:  ((s%16) d/32 + i/32) 4 + s/16
+ *   value scales at 66 d:  (((s/4)%4 d/32 + i/32) 4 + s/16) 4 + s%4
+ * so that one 16-byte load of a lane (8 bytes at d = 64) brings it what its
+ * matrix instructions take. The buffer is aligned to 16 bytes.
+ */
+
+/* Bytes of a 4-bit cache for B, Hkv, d and C of `shape` (0 if invalid). */
+size_t reskv_quant_cache_size(const reskv_shape_t* shape);
+
+/*
+ * reskv_pack_quant - write the live slots [0, res_len + main_len) of a cache
+ * kc, vc [B, Hkv, C, d] into a 4-bit cache. Other slots are left as they were.
+ */
+reskv_status_t reskv_pack_quant(const reskv_shape_t* shape, const void* kc, const void* vc,
+                                const int32_t* res_len, const int32_t* main_len,
+                                void* cache, void* stream);
+
+/*
+ * reskv_unpack_quant - the values a 4-bit cache stands for, in the shape's type
+ * (exact in both types, but for values below a type's normal range).
+ *   first_slot      [B*Hkv] int32, device, or NULL (0): the slot of row 0
+ *   n_rows          rows to read per (b, kv head), >= 0
+ *   kc, vc          out [B, Hkv, n_rows, d]: row i is slot first_slot + i; rows
+ *                   whose slot is not live are left as they were
+ */
+reskv_status_t reskv_unpack_quant(const reskv_shape_t* shape, const void* cache,
+                                  const int32_t* res_len, const int32_t* main_len,
+                                  const int32_t* first_slot, int32_t n_rows,
+                                  void* kc, void* vc, void* stream);
+
+/*
+ * reskv_append_kv_quant - append tokens to a 4-bit cache as main slots, the
+ * keys rotated by their positions on the way.
+ *   rope, positions the plan and [B, n_new] int32 (device) positions, or both
+ *                   NULL: keys as they are. Rotated keys are rounded to the
+ *                   shape's type, exactly as reskv_rope writes them, then coded
+ *   n_new           tokens per sequence, >= 0
+ *   n_tok           [B] int32, device, or NULL: tokens t >= n_tok[b] are
+ *                   padding and not appended
+ *   k_new, v_new    [B, Hkv, n_new, d]
+ *   main_len        advanced on the device by the tokens that were appended;
+ *                   tokens that find the cache full are dropped
+ * Equals reskv_pack_quant of the same rows bit for bit.
+ */
+reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rope_t* rope,
+                                     const int32_t* positions, int32_t n_new, const int32_t* n_tok,
+                                     const void* k_new, const void* v_new, void* cache,
+                                     const int32_t* res_len, int32_t* main_len, void* stream);
+
+/*
+ * reskv_decode_attn_quant - reskv_decode_attn over a 4-bit cache: the same
+ * computation (Sec. 5.4, Sec. 5.5.2, App. D, Algorithm 2) with every key and
+ * value the one its code stands for, taken exactly; q, k_new and v_new in the
+ * shape's type, everything else in 32 bits.
+ *   rope, positions a plan and [B] int32 (device) positions of this step's
+ *                   tokens, or both NULL: queries and the appended keys are
+ *                   rotated on the way, exactly as reskv_rope writes them
+ *   cache           4-bit cache
+ *   k_new, v_new    [B, Hkv, d] optional (both or neither): appended as by
+ *                   reskv_append_kv_quant before attending (the attention
+ *                   reads the values their codes stand for)
+ *   workspace       device scratch of reskv_decode_quant_workspace_size() bytes;
+ *                   calls sharing one must not overlap
+ *   other arguments, and what is written where, as for reskv_decode_attn
+ * A head without any live slot gives 0. Slots past res_len + main_len may hold
+ * anything, empty entries (logc = -inf) too.
+ */
+reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_gate_t* gate,
+                                       const reskv_rope_t* rope, const int32_t* positions,
+                                       const void* q, void* cache, const float* logc,
+                                       const int32_t* res_len, int32_t* main_len,
+                                       const void* k_new, const void* v_new, float* out,
+                                       float* dbg_lse_main, float* dbg_lse_res, float* dbg_gate,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace reskv_decode_attn_quant needs (0 if invalid). */
+size_t reskv_decode_quant_workspace_size(const reskv_shape_t* shape);
+
 /* Static description of a status code. */
 const char* reskv_status_string(reskv_status_t status);
 

@@ -245,6 +245,197 @@ reskv_status_t reskv_append_kv(const reskv_shape_t* shape, const void* k_new, co
   return ok();
 }
 
+// Row accesses move 16 bytes.
+static bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+reskv_status_t reskv_rope_init(const reskv_rope_params_t* p, reskv_rope_t* rope) {
+  if (!p || !rope) return fail(RESKV_ERR_INVALID_ARG, "params or rope is NULL");
+  if (p->rot_dim < 16 || p->rot_dim > 128 || p->rot_dim % 16 != 0)
+    return fail(RESKV_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [16, 128]", p->rot_dim);
+  if (p->layout != RESKV_ROPE_HALF && p->layout != RESKV_ROPE_INTERLEAVED)
+    return fail(RESKV_ERR_INVALID_ARG, "layout %d is neither HALF (0) nor INTERLEAVED (1)", p->layout);
+  if (p->scaling < RESKV_ROPE_NONE || p->scaling > RESKV_ROPE_YARN)
+    return fail(RESKV_ERR_INVALID_ARG, "scaling %d outside [0, 4]", p->scaling);
+  if (!(p->theta > 1.0) || !isfinite(p->theta)) return fail(RESKV_ERR_INVALID_ARG, "theta %g must be > 1", p->theta);
+  if (p->scaling != RESKV_ROPE_NONE && !(p->factor >= 1.0 && isfinite(p->factor)))
+    return fail(RESKV_ERR_INVALID_ARG, "factor %g must be >= 1", p->factor);
+  if (p->scaling >= RESKV_ROPE_LLAMA3 && !(p->original_len > 0.0 && isfinite(p->original_len)))
+    return fail(RESKV_ERR_INVALID_ARG, "original_len %g must be > 0", p->original_len);
+  if (p->scaling == RESKV_ROPE_LLAMA3 &&
+      !(p->low_freq_factor > 0.0 && p->high_freq_factor > p->low_freq_factor && isfinite(p->high_freq_factor)))
+    return fail(RESKV_ERR_INVALID_ARG, "frequency factors must satisfy 0 < low (%g) < high (%g)", p->low_freq_factor,
+                p->high_freq_factor);
+  if (p->scaling == RESKV_ROPE_YARN && !(p->beta_slow > 0.0 && p->beta_fast > p->beta_slow && isfinite(p->beta_fast)))
+    return fail(RESKV_ERR_INVALID_ARG, "betas must satisfy beta_fast (%g) > beta_slow (%g) > 0", p->beta_fast,
+                p->beta_slow);
+  if (!(p->attn_scale >= 0.0) || !isfinite(p->attn_scale))
+    return fail(RESKV_ERR_INVALID_ARG, "attn_scale %g must be >= 0", p->attn_scale);
+  make_rope(*p, rope);
+  return ok();
+}
+
+// A plan as reskv_rope_init leaves it, for rows of `shape`.
+static reskv_status_t check_rope(const reskv_shape_t* s, const reskv_rope_t* rope) {
+  if (rope->rot_dim < 16 || rope->rot_dim % 16 != 0 || rope->rot_dim > s->head_dim)
+    return fail(RESKV_ERR_INVALID_ARG, "rot_dim %d of the plan is not a multiple of 16 in [16, head_dim = %d]",
+                rope->rot_dim, s->head_dim);
+  if (rope->layout != RESKV_ROPE_HALF && rope->layout != RESKV_ROPE_INTERLEAVED)
+    return fail(RESKV_ERR_INVALID_ARG, "layout %d of the plan is neither HALF (0) nor INTERLEAVED (1)", rope->layout);
+  bool fine = isfinite(rope->attn_scale);
+  for (int i = 0; i < rope->rot_dim / 2; ++i) fine = fine && isfinite(rope->freq[i]);
+  if (!fine) return fail(RESKV_ERR_INVALID_ARG, "the plan holds numbers that are not finite");
+  return RESKV_OK;
+}
+
+// Input and output rows of one kind of heads.
+static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int heads, int n, const void* in,
+                                 const reskv_rows_t* from, void* out, const reskv_rows_t* to) {
+  if (!in && !out) return RESKV_OK;
+  if (!in || !out || !from || !to)
+    return fail(RESKV_ERR_INVALID_ARG, "%s needs its input, its output and the strides of both", name);
+  if (!aligned(in) || !aligned(out)) return fail(RESKV_ERR_INVALID_ARG, "%s pointers must be aligned to 16 bytes", name);
+  const int64_t unit = s->dtype == RESKV_BF16 ? 8 : 4, extent[3] = {s->batch, heads, n};
+  const int64_t* st[2] = {&from->batch, &to->batch};
+  int64_t span[2];  // elements from the first row's start to the last row's end
+  for (int k = 0; k < 2; ++k) {
+    span[k] = s->head_dim;
+    for (int i = 0; i < 3; ++i) {
+      if (extent[i] <= 1 && st[k][i] >= 0) continue;  // not used
+      if (st[k][i] < 0 || st[k][i] % unit != 0 || st[k][i] > ((int64_t)1 << 48) / (extent[i] - 1))
+        return fail(RESKV_ERR_INVALID_ARG, "%s stride %lld is not a multiple of 16 bytes >= 0 within 2^48 elements",
+                    name, (long long)st[k][i]);
+      span[k] += (extent[i] - 1) * st[k][i];
+    }
+  }
+  // output rows apart from each other: by rising stride, each passes what the ones before it span
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (st[1][order[j]] > st[1][order[j + 1]]) {
+        const int x = order[j];
+        order[j] = order[j + 1];
+        order[j + 1] = x;
+      }
+  int64_t used = s->head_dim;
+  for (int i = 0; i < 3; ++i) {
+    const int o = order[i];
+    if (extent[o] <= 1) continue;
+    if (st[1][o] < used) return fail(RESKV_ERR_INVALID_ARG, "%s output rows overlap", name);
+    used += (extent[o] - 1) * st[1][o];
+  }
+  bool same = in == out;
+  for (int i = 0; i < 3; ++i) same = same && (extent[i] <= 1 || st[0][i] == st[1][i]);
+  const uintptr_t e = 16 / unit, i0 = (uintptr_t)in, o0 = (uintptr_t)out;
+  if (!same && i0 < o0 + span[1] * e && o0 < i0 + span[0] * e)
+    return fail(RESKV_ERR_INVALID_ARG, "%s output overlaps its input without being it", name);
+  return RESKV_OK;
+}
+
+reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, int32_t n_rows,
+                          const int32_t* positions, const int32_t* n_tok, const void* q, const reskv_rows_t* q_at,
+                          void* q_out, const reskv_rows_t* q_out_at, const void* k, const reskv_rows_t* k_at,
+                          void* k_out, const reskv_rows_t* k_out_at, void* stream) {
+  reskv_status_t st = check_shape(shape);
+  if (st != RESKV_OK) return st;
+  if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
+  if (n_rows == 0) return ok();  // tensors without elements may have no address
+  if (!rope || !positions) return fail(RESKV_ERR_INVALID_ARG, "rope or positions is NULL");
+  if ((st = check_rope(shape, rope)) != RESKV_OK) return st;
+  if (!q && !q_out && !k && !k_out) return fail(RESKV_ERR_INVALID_ARG, "neither queries nor keys are given");
+  if ((st = check_rows(shape, "q", shape->num_q_heads, n_rows, q, q_at, q_out, q_out_at)) != RESKV_OK) return st;
+  if ((st = check_rows(shape, "k", shape->num_kv_heads, n_rows, k, k_at, k_out, k_out_at)) != RESKV_OK) return st;
+  hipError_t e = launch_rope(*shape, *rope, n_rows, positions, n_tok, q, q_at, q_out, q_out_at, k, k_at, k_out,
+                             k_out_at, (hipStream_t)stream);
+  if (e != hipSuccess) return fail(RESKV_ERR_HIP, "rope launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+size_t reskv_quant_cache_size(const reskv_shape_t* shape) {
+  return check_shape(shape) == RESKV_OK ? quant_cache_bytes(*shape) : 0;
+}
+
+reskv_status_t reskv_pack_quant(const reskv_shape_t* shape, const void* kc, const void* vc, const int32_t* res_len,
+                                const int32_t* main_len, void* cache, void* stream) {
+  reskv_status_t st = check_shape(shape);
+  if (st != RESKV_OK) return st;
+  if (!kc || !vc || !res_len || !main_len || !cache) return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!aligned(kc) || !aligned(vc) || !aligned(cache))
+    return fail(RESKV_ERR_INVALID_ARG, "kc, vc and cache must be aligned to 16 bytes");
+  hipError_t e = launch_pack_quant(*shape, kc, vc, res_len, main_len, cache, (hipStream_t)stream);
+  if (e != hipSuccess) return fail(RESKV_ERR_HIP, "pack launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+reskv_status_t reskv_unpack_quant(const reskv_shape_t* shape, const void* cache, const int32_t* res_len,
+                                  const int32_t* main_len, const int32_t* first_slot, int32_t n_rows, void* kc,
+                                  void* vc, void* stream) {
+  reskv_status_t st = check_shape(shape);
+  if (st != RESKV_OK) return st;
+  if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
+  if (n_rows == 0) return ok();
+  if (!cache || !res_len || !main_len || !kc || !vc) return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!aligned(kc) || !aligned(vc) || !aligned(cache))
+    return fail(RESKV_ERR_INVALID_ARG, "kc, vc and cache must be aligned to 16 bytes");
+  hipError_t e = launch_unpack_quant(*shape, cache, res_len, main_len, first_slot, n_rows, kc, vc,
+                                     (hipStream_t)stream);
+  if (e != hipSuccess) return fail(RESKV_ERR_HIP, "unpack launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// Rotation arguments of the calls where it is optional.
+static reskv_status_t check_turn(const reskv_shape_t* shape, const reskv_rope_t* rope, const int32_t* positions) {
+  if ((rope == nullptr) != (positions == nullptr))
+    return fail(RESKV_ERR_INVALID_ARG, "rope and positions must both be given or both be NULL");
+  return rope ? check_rope(shape, rope) : RESKV_OK;
+}
+
+reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rope_t* rope, const int32_t* positions,
+                                     int32_t n_new, const int32_t* n_tok, const void* k_new, const void* v_new,
+                                     void* cache, const int32_t* res_len, int32_t* main_len, void* stream) {
+  reskv_status_t st = check_shape(shape);
+  if (st != RESKV_OK) return st;
+  if (n_new < 0) return fail(RESKV_ERR_INVALID_ARG, "n_new %d must be >= 0", n_new);
+  if (n_new == 0) return ok();
+  if (!k_new || !v_new || !cache || !res_len || !main_len)
+    return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
+  if ((st = check_turn(shape, rope, positions)) != RESKV_OK) return st;
+  if (!aligned(k_new) || !aligned(v_new) || !aligned(cache))
+    return fail(RESKV_ERR_INVALID_ARG, "k_new, v_new and cache must be aligned to 16 bytes");
+  hipError_t e = launch_append_quant(*shape, rope, positions, n_new, n_tok, k_new, v_new, cache, res_len, main_len,
+                                     (hipStream_t)stream);
+  if (e != hipSuccess) return fail(RESKV_ERR_HIP, "append launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+size_t reskv_decode_quant_workspace_size(const reskv_shape_t* shape) {
+  return check_shape(shape) == RESKV_OK ? make_quant_decode_plan(*shape).bytes : 0;
+}
+
+reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_gate_t* gate, const reskv_rope_t* rope,
+                                       const int32_t* positions, const void* q, void* cache, const float* logc,
+                                       const int32_t* res_len, int32_t* main_len, const void* k_new,
+                                       const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
+                                       float* dbg_gate, void* workspace, size_t workspace_bytes, void* stream) {
+  reskv_status_t st = check_shape(shape);
+  if (st != RESKV_OK) return st;
+  if ((st = check_gate(gate)) != RESKV_OK) return st;
+  if (!q || !cache || !logc || !res_len || !main_len || !out)
+    return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
+  if ((st = check_turn(shape, rope, positions)) != RESKV_OK) return st;
+  if ((k_new == nullptr) != (v_new == nullptr))
+    return fail(RESKV_ERR_INVALID_ARG, "k_new and v_new must both be given or both be NULL");
+  if (!aligned(q) || !aligned(cache) || !aligned(k_new) || !aligned(v_new))
+    return fail(RESKV_ERR_INVALID_ARG, "q, k_new, v_new and cache must be aligned to 16 bytes");
+  const QuantDecodePlan plan = make_quant_decode_plan(*shape);
+  if (!workspace || workspace_bytes < plan.bytes)
+    return fail(RESKV_ERR_WORKSPACE, "decode needs %zu workspace bytes, got %zu", plan.bytes,
+                workspace ? workspace_bytes : (size_t)0);
+  hipError_t e = launch_decode_quant(*shape, *gate, plan, rope, positions, q, cache, logc, res_len, main_len, k_new,
+                                     v_new, out, dbg_lse_main, dbg_lse_res, dbg_gate, workspace, (hipStream_t)stream);
+  if (e != hipSuccess) return fail(RESKV_ERR_HIP, "decode launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
 static reskv_status_t check_build(const reskv_shape_t* shape, const reskv_build_params_t* p,
                                   const int32_t* seq_len, const int32_t* budget, const int32_t* res_count) {
   reskv_status_t st = check_shape(shape);

@@ -103,6 +103,14 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) {
   return x < lo ? lo : (x > hi ? hi : x);
 }
 
+// Lengths of a (b, kv head) cache clamped to its capacities, so corrupt lengths
+// cannot make a kernel read outside it.
+__device__ __forceinline__ void cache_lengths(const int32_t* res_len, const int32_t* main_len,
+                                              int bh, int C, int Rcap, int& r, int& n) {
+  r = clampi(res_len[bh], 0, min(Rcap, C));
+  n = clampi(main_len[bh], 0, C - r);
+}
+
 // ---- 16x16 MFMA tiles over a full row of D elements ------------------------
 // C[16 x 16] = A[16 x D] . B[16 x D]^T. Lane l supplies A row (l % 16) and B
 // row (l % 16); lane group g = l / 16 takes the 16-byte pieces g, g + 4,

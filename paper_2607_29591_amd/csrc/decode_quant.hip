@@ -1,0 +1,450 @@
+// Shared-softmax residual decode (Sec. 5.4; Sec. 5.5.2 gate; App. D, Algorithm 2)
+// over a cache held in 4 bits.
+//
+// One block of 8 waves per (b, kv head); a wave takes blocks of 64 slots (the
+// cache's own blocks) and keeps a running maximum, sum and output per query head
+// for the residual slots, then for the main slots; the waves' states are merged
+// in LDS, where the gate joins the two kinds. With hd = lane % 16, g = lane / 16:
+//   * logits S^T = K Q^T per 16-slot tile t: lane (hd, g) loads D / 4 elements
+//     of key row 16t + hd (16 bytes at D = 128), all of one scale, which the
+//     conversion applies: every code times its scale is a bf16 number, so the
+//     matrix instruction gets exact operands. The contraction index of step i,
+//     lane group g stands for elements g D/4 + 8i .. + 7 on both sides. The lane
+//     ends with the logits of slots 16t + 4g + i' of head hd, in base 2 with
+//     log2(e) / sqrt(d) in the scale.
+//   * O^T += V^T P^T: lane (m, g) loads the m-th piece (D / 16 elements) of value
+//     rows 16T + 4g + u, u = 0..3, in one load per T; contraction index 8g + i'
+//     of step h stands for slot 16(2h + i'/4) + 4g + i'%4, so the B operand is
+//     the lane's own probabilities, as bf16 hi + lo parts, each rounded to
+//     nearest (together 2^-18 of the probability).
+// fp32 queries enter as three bf16 parts, which hold all of their 24 bits.
+#include "internal.h"
+#include "quant.h"
+#include "rotate.h"
+
+namespace reskv {
+
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kUnit = 64;  // slots of a cache block
+constexpr int kTiles = kUnit / 16;
+
+struct QuantDecodeArgs {
+  reskv_rope_t rope;
+  const int32_t* positions;  // NULL: no rotation
+  const void* q;
+  uint8_t* cache;
+  const float* logc;
+  const int32_t* res_len;
+  int32_t* main_len;
+  const void* k_new;  // appended first, or NULL
+  const void* v_new;
+  const float* tau;
+  float* out;
+  float* dbg_lse_main;
+  float* dbg_lse_res;
+  float* dbg_gate;
+  int Hq, Hkv, G, C, Rcap, NB;
+  float qk_scale;   // log2(e) / sqrt(d)
+  float beta_log2;  // beta * log2(e)
+  float tau_scalar, alpha, g_min;
+};
+
+template <int kBytes>
+struct Words;
+template <>
+struct Words<16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  }
+};
+template <>
+struct Words<8> {
+  uint32_t w[2];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x; w[1] = x.y;
+  }
+};
+
+// One block of 64 slots in registers.
+template <int D>
+struct Unit {
+  Words<D / 8> k[kTiles];  // key codes of row 16t + hd, elements g D/4 ..
+  uint32_t ks;             // their scales, byte t
+  Words<D / 8> v[kTiles];  // value codes of piece hd, rows 16T + 4g + u
+  Words<16> vs;            // their scales, word T, byte u
+  __device__ __forceinline__ void load(const uint8_t* block, int hd, int g) {
+    using Q = QuantBlock<D>;
+    constexpr int kLanes = 4 / Q::kGroups;  // lane groups of one key scale
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) k[t].load(block + Q::k_code(16 * t + hd) + g * (D / 8));
+    ks = *reinterpret_cast<const uint32_t*>(block + Q::k_scale(hd, g / kLanes));
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) v[t].load(block + Q::v_code(16 * t + 4 * g, hd));
+    vs.load(block + Q::v_scale(4 * g, hd * Q::kPiece / 32));
+  }
+};
+
+template <int kByte>
+__device__ __forceinline__ float byte_scale(uint32_t w) {
+  return scale_of((w >> (8 * kByte)) & 0xffu);
+}
+
+// A row fragment: elements g D/4 .. (g + 1) D/4 of one row as bf16 pairs, D / 32
+// matrix steps of 8 elements.
+template <int D>
+struct Row {
+  uint4 s[D / 32];
+};
+
+// 8 codes of a word as 8 bf16 numbers.
+__device__ __forceinline__ uint4 eight(uint32_t codes, float scale) {
+  return make_uint4(value_pair<0>(codes, scale), value_pair<1>(codes, scale), value_pair<2>(codes, scale),
+                    value_pair<3>(codes, scale));
+}
+
+template <int D, int NP>
+__device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[NP], float qk_scale,
+                                            float (&s)[kTiles][4]) {
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const float scale = t == 0 ? byte_scale<0>(u.ks) : t == 1 ? byte_scale<1>(u.ks)
+                      : t == 2 ? byte_scale<2>(u.ks) : byte_scale<3>(u.ks);
+    f32x4_t c = zero4();
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const bf16x8_t k = as_bf16x8(eight(u.k[t].w[i], scale));
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p)  // the smallest part first
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16x8(q[p].s[i]), c, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[t][i] = c[i] * qk_scale;
+  }
+}
+
+// Running state of one kind of slots: head hd's maximum and sum (the same in
+// the four lane groups), and O[hd][(D/16)(4g + i) + e] in acc[e][i].
+template <int D>
+struct State {
+  static constexpr int kE = D / 16;
+  float m, l;
+  f32x4_t acc[kE];
+  __device__ void reset() {
+    m = kNegInf;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) acc[e] = zero4();
+  }
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
+}
+
+// O^T += V^T P^T for the unit; rows without weight must hold finite numbers.
+template <int D>
+__device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const float (&vs)[kTiles][4],
+                                        const float (&p)[kTiles][4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t bh[4], bl[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float pa = p[2 * h + w / 2][2 * (w % 2)], pb = p[2 * h + w / 2][2 * (w % 2) + 1];
+      bh[w] = pack_bf16(pa, pb);
+      bl[w] = pack_bf16(pa - bf16_lo(bh[w]), pb - bf16_hi(bh[w]));
+    }
+    const bf16x8_t Bh = as_bf16x8(make_uint4(bh[0], bh[1], bh[2], bh[3]));
+    const bf16x8_t Bl = as_bf16x8(make_uint4(bl[0], bl[1], bl[2], bl[3]));
+    // element pair e, e + 1 of the 8 rows of this step
+    auto step = [&](int e, const uint32_t (&x)[8]) {
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const uint32_t sel = o ? 0x07060302u : 0x05040100u;
+        uint32_t a[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) a[w] = __builtin_amdgcn_perm(x[2 * w + 1], x[2 * w], sel);
+        const bf16x8_t A = as_bf16x8(make_uint4(a[0], a[1], a[2], a[3]));
+        st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bh, st.acc[e + o], 0, 0, 0);
+        st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bl, st.acc[e + o], 0, 0, 0);
+      }
+    };
+    uint32_t x[8];
+    if constexpr (D == 128) {  // a word per row
+#define RESKV_PAIRS(B)                                                                       \
+  {                                                                                          \
+    _Pragma("unroll") for (int k = 0; k < 8; ++k) x[k] =                                     \
+        value_pair<B>(u.v[2 * h + k / 4].w[k % 4], vs[2 * h + k / 4][k % 4]);                \
+    step(2 * B, x);                                                                          \
+  }
+      RESKV_PAIRS(0) RESKV_PAIRS(1) RESKV_PAIRS(2) RESKV_PAIRS(3)
+#undef RESKV_PAIRS
+    } else {  // half a word per row
+#define RESKV_PAIRS(B)                                                                       \
+  {                                                                                          \
+    _Pragma("unroll") for (int k = 0; k < 8; k += 2) {                                       \
+      x[k] = value_pair<B>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[2 * h + k / 4][k % 4]);       \
+      x[k + 1] = value_pair<B + 2>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[2 * h + k / 4][k % 4 + 1]); \
+    }                                                                                        \
+    step(2 * B, x);                                                                          \
+  }
+      RESKV_PAIRS(0) RESKV_PAIRS(1)
+#undef RESKV_PAIRS
+    }
+  }
+}
+
+// Online softmax over the unit's slots [lo, hi) of one kind. Residual slots add
+// beta * log2 count; slots of no weight (outside, empty entries) get zero
+// probability and a zero scale, so whatever their codes say does not enter.
+template <int D>
+__device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const float (&s)[kTiles][4],
+                                           const float (&lc)[kTiles][4], int lo, int hi, bool is_res,
+                                           float beta_log2, int g) {
+  float p[kTiles][4], vs[kTiles][4];
+  float top = kNegInf;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    vs[t][0] = byte_scale<0>(u.vs.w[t]);
+    vs[t][1] = byte_scale<1>(u.vs.w[t]);
+    vs[t][2] = byte_scale<2>(u.vs.w[t]);
+    vs[t][3] = byte_scale<3>(u.vs.w[t]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = 16 * t + 4 * g + i;
+      const bool live = j >= lo && j < hi && !(is_res && lc[t][i] == kNegInf);
+      const float v = is_res ? fmaf(beta_log2, lc[t][i], s[t][i]) : s[t][i];
+      p[t][i] = live ? v : kNegInf;
+      vs[t][i] = live ? vs[t][i] : 0.f;
+      top = fmaxf(top, p[t][i]);
+    }
+  }
+  top = rows4_max(top);
+  const float m_new = fmaxf(st.m, top);
+  const float mu = m_new == kNegInf ? 0.f : m_new;
+  const float alpha = fast_exp2(st.m - mu);
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[t][i] = fast_exp2(p[t][i] - mu);
+      sum += p[t][i];
+    }
+  sum = rows4_sum(sum);
+  st.l = fmaf(st.l, alpha, sum);
+  st.m = m_new;
+#pragma unroll
+  for (int e = 0; e < State<D>::kE; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st.acc[e][i] *= alpha;
+  pv_unit<D>(st, u, vs, p);
+}
+
+template <int D, int GP>
+__device__ __forceinline__ void store_state(const State<D>& st, float (*acc)[D], float* m, float* l, int hd, int g) {
+  if (hd >= GP) return;
+  constexpr int kE = D / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) acc[hd][kE * (4 * g + i) + e] = st.acc[e][i];
+  if (g == 0) {
+    m[hd] = st.m;
+    l[hd] = st.l;
+  }
+}
+
+template <typename T, int D, int GP>
+__global__ __launch_bounds__(kThreads) void decode_quant_head(QuantDecodeArgs a) {
+  using Q = QuantBlock<D>;
+  constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+  const int bh = blockIdx.x, b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int hd = lane & 15, g = lane >> 4;
+  uint8_t* cache = a.cache + (size_t)bh * a.NB * Q::kBytes;
+  const float* logc = a.logc + (size_t)bh * a.Rcap;
+
+  __shared__ float s_acc[2][kWaves][GP][D];
+  __shared__ float s_m[2][kWaves][GP];  // per kind (0 residual, 1 main), per wave
+  __shared__ float s_l[2][kWaves][GP];
+  __shared__ __align__(16) uint16_t s_q[NP][GP][D];
+  __shared__ double2 s_cs[64];
+
+  int r, n;
+  cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
+  const bool app = a.k_new != nullptr && r + n < a.C;
+  const int app_slot = r + n;
+  if (app) n += 1;
+  const int rot = a.positions ? a.rope.rot_dim : 0;
+  if (tid < rot / 2) s_cs[tid] = turn(a.rope.freq[tid], a.positions[b], a.rope.attn_scale);
+  __syncthreads();
+  // this step's token into the cache (wave 0 the key, wave 1 the value)
+  if (app && wave < 2) {
+    const T* src = static_cast<const T*>(wave ? a.v_new : a.k_new) + (size_t)bh * D;
+    const int l = min(lane, D / 2 - 1), rk = wave ? 0 : rot;
+    store_row_quant<D>(cache + (size_t)(app_slot / kUnit) * Q::kBytes, app_slot % kUnit, wave == 1,
+                       rotated_elem(src, 2 * l, rk, a.rope.layout, s_cs),
+                       rotated_elem(src, 2 * l + 1, rk, a.rope.layout, s_cs), lane);
+  }
+  // queries, rotated, as bf16 parts
+  for (int i = tid; i < GP * D; i += kThreads) {
+    const int h = i / D, e = i % D;
+    float x = 0.f;
+    if (h < a.G)
+      x = rotated_elem(static_cast<const T*>(a.q) + ((size_t)b * a.Hq + (size_t)kvh * a.G + h) * D, e, rot,
+                       a.rope.layout, s_cs);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const uint16_t w = f32_to_bf16_rne(x);
+      s_q[p][h][e] = w;
+      x -= __uint_as_float((uint32_t)w << 16);
+    }
+  }
+  __syncthreads();
+  Row<D> q[NP];
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      q[p].s[i] = hd < GP ? *reinterpret_cast<const uint4*>(&s_q[p][hd][g * (D / 4) + 8 * i]) : make_uint4(0, 0, 0, 0);
+
+  // Work list: the blocks that hold residual slots, then those that hold main
+  // slots (the block of slot r, if both, in both parts), dealt to the waves in
+  // turn, so that a wave meets its residual blocks first.
+  const int total = r + n;
+  const int UR = (r + kUnit - 1) / kUnit, first_main = r / kUnit;
+  const int U = UR + (n > 0 ? (total + kUnit - 1) / kUnit - first_main : 0);
+  State<D> st;
+  st.reset();
+  bool in_res = true;
+  for (int p = wave; p < U; p += kWaves) {
+    const bool is_res = p < UR;
+    if (!is_res && in_res) {
+      store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
+      st.reset();
+      in_res = false;
+    }
+    const int blk = is_res ? p : first_main + p - UR;
+    const int lo = is_res ? 0 : r - blk * kUnit, hi = (is_res ? r : total) - blk * kUnit;
+    Unit<D> u;
+    u.load(cache + (size_t)blk * Q::kBytes, hd, g);
+    float lc[kTiles][4] = {};
+    if (is_res) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 16 * t + 4 * g + i;
+          lc[t][i] = j < hi ? logc[blk * kUnit + j] : 0.f;
+        }
+    }
+    float s[kTiles][4];
+    unit_logits<D, NP>(u, q, a.qk_scale, s);
+    softmax_pv<D>(st, u, s, lc, lo, hi, is_res, a.beta_log2, g);
+  }
+  if (in_res) {
+    store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
+    st.reset();
+  }
+  store_state<D, GP>(st, s_acc[1][wave], s_m[1][wave], s_l[1][wave], hd, g);
+  __syncthreads();
+
+  // (head h, column d) of one kind over the waves
+  auto merge = [&](int kind, int h, int d, float& M, float& l, float& o) {
+    M = s_m[kind][0][h];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[kind][w][h]);
+    o = 0.f;
+    l = 0.f;
+    if (M != kNegInf) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2f(s_m[kind][w][h] - M);
+        o = fmaf(f, s_acc[kind][w][h][d], o);
+        l = fmaf(f, s_l[kind][w][h], l);
+      }
+    }
+  };
+  for (int i = tid; i < a.G * D; i += kThreads) {
+    const int h = i / D, d = i % D;
+    float mR, lR, oR, mM, lM, oM;
+    merge(0, h, d, mR, lR, oR);
+    merge(1, h, d, mM, lM, oM);
+    const int qh = b * a.Hq + kvh * a.G + h;
+    const float tau = a.tau ? a.tau[qh] : a.tau_scalar;
+    // p_max = 1 / l_main (the largest term is exactly 1), then the gate
+    const float pmax = lM > 0.f ? 1.f / lM : 1.f;
+    const float gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
+    const float lg = gate > 0.f ? log2f(gate) : kNegInf;
+    const float mRg = (mR == kNegInf || lg == kNegInf) ? kNegInf : mR + lg;
+    const float M = fmaxf(mM, mRg);
+    const float fM = mM != kNegInf ? exp2f(mM - M) : 0.f;
+    const float fR = mRg != kNegInf ? exp2f(mRg - M) : 0.f;
+    const float den = lM * fM + lR * fR;
+    const float num = oM * fM + oR * fR;
+    a.out[(size_t)qh * D + d] = den != 0.f ? num / den : 0.f;  // NaN stays NaN
+    if (d == 0) {
+      if (a.dbg_lse_main) a.dbg_lse_main[qh] = lM != 0.f ? (mM + log2f(lM)) * kLn2 : kNegInf;
+      if (a.dbg_lse_res) a.dbg_lse_res[qh] = lR != 0.f ? (mR + log2f(lR)) * kLn2 : kNegInf;
+      if (a.dbg_gate) a.dbg_gate[qh] = gate;
+    }
+  }
+  if (app && tid == 0) a.main_len[bh] = n;
+}
+
+template <typename T, int D>
+hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStream_t stream) {
+  const dim3 grid(pl.BH), block(kThreads);
+  switch (pl.GP) {
+    case 1: hipLaunchKernelGGL((decode_quant_head<T, D, 1>), grid, block, 0, stream, da); break;
+    case 2: hipLaunchKernelGGL((decode_quant_head<T, D, 2>), grid, block, 0, stream, da); break;
+    case 4: hipLaunchKernelGGL((decode_quant_head<T, D, 4>), grid, block, 0, stream, da); break;
+    case 8: hipLaunchKernelGGL((decode_quant_head<T, D, 8>), grid, block, 0, stream, da); break;
+    default: hipLaunchKernelGGL((decode_quant_head<T, D, 16>), grid, block, 0, stream, da); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
+  QuantDecodePlan p{};
+  p.BH = s.batch * s.num_kv_heads;
+  const int G = s.num_q_heads / s.num_kv_heads;
+  p.GP = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : G <= 8 ? 8 : 16;
+  p.bytes = 256;
+  return p;
+}
+
+hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, const QuantDecodePlan& pl,
+                               const reskv_rope_t* rope, const int32_t* positions, const void* q, void* cache,
+                               const float* logc, const int32_t* res_len, int32_t* main_len, const void* k_new,
+                               const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
+                               float* dbg_gate, void* workspace, hipStream_t stream) {
+  (void)workspace;
+  QuantDecodeArgs da{};
+  if (rope) da.rope = *rope;
+  da.positions = rope ? positions : nullptr;
+  da.q = q; da.cache = (uint8_t*)cache; da.logc = logc;
+  da.res_len = res_len; da.main_len = main_len; da.k_new = k_new; da.v_new = v_new;
+  da.tau = g.tau; da.out = out;
+  da.dbg_lse_main = dbg_lse_main; da.dbg_lse_res = dbg_lse_res; da.dbg_gate = dbg_gate;
+  da.Hq = s.num_q_heads; da.Hkv = s.num_kv_heads; da.G = s.num_q_heads / s.num_kv_heads;
+  da.C = s.slot_cap; da.Rcap = s.res_cap; da.NB = (s.slot_cap + kUnit - 1) / kUnit;
+  da.qk_scale = kLog2e / sqrtf((float)s.head_dim);
+  da.beta_log2 = g.beta * kLog2e;
+  da.tau_scalar = g.tau_scalar; da.alpha = g.alpha; da.g_min = g.g_min;
+  const bool bf = s.dtype == RESKV_BF16;
+  if (s.head_dim == 128) return bf ? launch_gp<uint16_t, 128>(pl, da, stream) : launch_gp<float, 128>(pl, da, stream);
+  return bf ? launch_gp<uint16_t, 64>(pl, da, stream) : launch_gp<float, 64>(pl, da, stream);
+}
+
+}  // namespace reskv

@@ -65,6 +65,35 @@ hipError_t launch_merge_branches(const reskv_shape_t& s, int mode, const float* 
 hipError_t launch_append(const reskv_shape_t& s, const void* k_new, const void* v_new, void* kc,
                          void* vc, const int32_t* res_len, int32_t* main_len, hipStream_t stream);
 
+// Rotary positions.
+void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope);
+hipError_t launch_rope(const reskv_shape_t& s, const reskv_rope_t& rope, int n_rows, const int32_t* positions,
+                       const int32_t* n_tok, const void* q, const reskv_rows_t* q_at, void* q_out,
+                       const reskv_rows_t* q_out_at, const void* k, const reskv_rows_t* k_at, void* k_out,
+                       const reskv_rows_t* k_out_at, hipStream_t stream);
+
+// Caches in 4 bits.
+size_t quant_cache_bytes(const reskv_shape_t& s);
+hipError_t launch_pack_quant(const reskv_shape_t& s, const void* kc, const void* vc, const int32_t* res_len,
+                             const int32_t* main_len, void* cache, hipStream_t stream);
+hipError_t launch_unpack_quant(const reskv_shape_t& s, const void* cache, const int32_t* res_len,
+                               const int32_t* main_len, const int32_t* first, int n_rows, void* kc, void* vc,
+                               hipStream_t stream);
+hipError_t launch_append_quant(const reskv_shape_t& s, const reskv_rope_t* rope, const int32_t* positions, int n_new,
+                               const int32_t* n_tok, const void* k_new, const void* v_new, void* cache,
+                               const int32_t* res_len, int32_t* main_len, hipStream_t stream);
+
+struct QuantDecodePlan {
+  int BH, GP;
+  size_t bytes;
+};
+QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s);
+hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, const QuantDecodePlan& pl,
+                               const reskv_rope_t* rope, const int32_t* positions, const void* q, void* cache,
+                               const float* logc, const int32_t* res_len, int32_t* main_len, const void* k_new,
+                               const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
+                               float* dbg_gate, void* workspace, hipStream_t stream);
+
 // Which kernels a decode call of these sizes takes, for the tests and the
 // benchmark's labels (not part of the C ABI): entry 0 reskv_decode_attn, 1
 // reskv_decode_branches, 2 reskv_decode_attn_ragged with the workspace its

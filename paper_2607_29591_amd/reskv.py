@@ -45,6 +45,22 @@ class ProxyParams(ctypes.Structure):
                 ("val_rows", ctypes.c_int32), ("delta", ctypes.c_float)]
 
 
+class RopeParams(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("theta", ctypes.c_double), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low_freq_factor", ctypes.c_double), ("high_freq_factor", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("attn_scale", ctypes.c_double)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("attn_scale", ctypes.c_double),
+                ("freq", ctypes.c_double * 64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
 class Gate(ctypes.Structure):
     _fields_ = [("tau", ctypes.c_void_p), ("tau_scalar", ctypes.c_float),
                 ("alpha", ctypes.c_float), ("g_min", ctypes.c_float), ("beta", ctypes.c_float)]
@@ -80,6 +96,18 @@ _SIG = {
                                              _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "reskv_merge_branches": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P]),
     "reskv_append_kv": (ctypes.c_int, [ctypes.POINTER(Shape), _P, _P, _P, _P, _P, _P, _P]),
+    "reskv_rope_init": (ctypes.c_int, [ctypes.POINTER(RopeParams), ctypes.POINTER(Rope)]),
+    "reskv_rope": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.c_int32, _P, _P, _P,
+                                  ctypes.POINTER(Rows), _P, ctypes.POINTER(Rows), _P, ctypes.POINTER(Rows), _P,
+                                  ctypes.POINTER(Rows), _P]),
+    "reskv_quant_cache_size": (ctypes.c_size_t, [ctypes.POINTER(Shape)]),
+    "reskv_pack_quant": (ctypes.c_int, [ctypes.POINTER(Shape), _P, _P, _P, _P, _P, _P]),
+    "reskv_unpack_quant": (ctypes.c_int, [ctypes.POINTER(Shape), _P, _P, _P, _P, ctypes.c_int32, _P, _P, _P]),
+    "reskv_append_kv_quant": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), _P, ctypes.c_int32, _P, _P,
+                                             _P, _P, _P, _P, _P]),
+    "reskv_decode_attn_quant": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.POINTER(Gate), ctypes.POINTER(Rope), _P,
+                                               _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "reskv_decode_quant_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(Shape)]),
     "reskv_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "reskv_last_error": (ctypes.c_char_p, []),
 }
@@ -314,6 +342,176 @@ def reskv_merge_branches(shape, mode, out_main, lse_main, out_res, lse_res, gate
 def reskv_append_kv(shape, k_new, v_new, kc, vc, res_len, main_len, stream=None):
     _check(lib().reskv_append_kv(ctypes.byref(shape), _ptr(k_new), _ptr(v_new), _ptr(kc), _ptr(vc),
                                  _ptr(res_len), _ptr(main_len), _stream(stream)))
+
+
+# ------------------------------------- rotary positions, caches in 4 bits
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "llama3": 3, "yarn": 4}
+
+
+def make_rope(rot_dim, layout="half", theta=10000.0, scaling="none", factor=1.0, original_len=0.0,
+              low_freq_factor=1.0, high_freq_factor=4.0, beta_fast=32.0, beta_slow=1.0, attn_scale=0.0):
+    """Rotation plan (reskv_rope_init); attn_scale 0 takes the scaling's own factor."""
+    p = RopeParams(rot_dim, ROPE_LAYOUTS.get(layout, layout), ROPE_SCALINGS.get(scaling, scaling), theta, factor,
+                   original_len, low_freq_factor, high_freq_factor, beta_fast, beta_slow, attn_scale)
+    rope = Rope()
+    _check(lib().reskv_rope_init(ctypes.byref(p), ctypes.byref(rope)))
+    return rope
+
+
+def _tensor(name, t, dtype, count, contiguous=True):
+    """Pointer of a tensor of the current GPU with `count` elements of `dtype` (None -> NULL)."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() != count:
+        raise ValueError(f"{name} must have {count} elements, got {tuple(t.shape)}")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU, got {t.device}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _dtype(shape):
+    import torch
+    return torch.bfloat16 if shape.dtype == RESKV_BF16 else torch.float32
+
+
+def _prepared(fn, args, keep):
+    """Function that issues fn(*args); `keep` lives as long as it does."""
+    def call():
+        status = fn(*args)
+        if status != 0:
+            _check(status)
+
+    call.keep = keep
+    return call
+
+
+def prepare_rope(shape, rope, positions, q=None, q_out=None, k=None, k_out=None, n_tok=None, stream=None):
+    """Marshal one reskv_rope call once and return a function that issues it (for loops that launch the same
+    calls many times). The caller keeps the tensors alive and unchanged in place."""
+    import torch
+    B, d, n = shape.batch, shape.head_dim, int(positions.shape[-1]) if positions.dim() > 1 else 1
+    at = []
+    for name, x, heads in (("q", q, shape.num_q_heads), ("q_out", q_out, shape.num_q_heads),
+                           ("k", k, shape.num_kv_heads), ("k_out", k_out, shape.num_kv_heads)):
+        if x is None:
+            at += [None, None]
+            continue
+        if tuple(x.shape) != (B, heads, n, d) or x.stride(3) != 1:
+            raise ValueError(f"{name} must be [{B}, {heads}, {n}, {d}] with adjoining elements, got {tuple(x.shape)} "
+                             f"by {x.stride()}")
+        at += [_tensor(name, x, _dtype(shape), x.numel(), False), ctypes.byref(Rows(*x.stride()[:3]))]
+    args = (ctypes.byref(shape), ctypes.byref(rope), n, _tensor("positions", positions, torch.int32, B * n),
+            _tensor("n_tok", n_tok, torch.int32, B), *at, _stream(stream))
+    return _prepared(lib().reskv_rope, args, (shape, rope))
+
+
+def reskv_rope(shape, rope, positions, q=None, q_out=None, k=None, k_out=None, n_tok=None, stream=None):
+    """Rotate q [B, Hq, n, d] and / or k [B, Hkv, n, d] (any strides: pass a transposed view of a token-major
+    tensor) into q_out, k_out by positions [B, n]; rows from n_tok [B] on are left as they were."""
+    prepare_rope(shape, rope, positions, q, q_out, k, k_out, n_tok, stream)()
+
+
+def reskv_quant_cache_size(shape):
+    return lib().reskv_quant_cache_size(ctypes.byref(shape))
+
+
+def _quant_lens(shape, cache, res_len, main_len):
+    import torch
+    pairs = shape.batch * shape.num_kv_heads
+    return (_tensor("cache", cache, torch.uint8, reskv_quant_cache_size(shape)),
+            _tensor("res_len", res_len, torch.int32, pairs), _tensor("main_len", main_len, torch.int32, pairs))
+
+
+def prepare_pack_quant(shape, kc, vc, res_len, main_len, cache, stream=None):
+    """As prepare_rope, for reskv_pack_quant."""
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
+    count = shape.batch * shape.num_kv_heads * shape.slot_cap * shape.head_dim
+    args = (ctypes.byref(shape), _tensor("kc", kc, _dtype(shape), count), _tensor("vc", vc, _dtype(shape), count),
+            rl, ml, c, _stream(stream))
+    return _prepared(lib().reskv_pack_quant, args, (shape,))
+
+
+def reskv_pack_quant(shape, kc, vc, res_len, main_len, cache, stream=None):
+    """Live slots of kc, vc [B, Hkv, C, d] into the 4-bit cache (uint8, reskv_quant_cache_size bytes)."""
+    prepare_pack_quant(shape, kc, vc, res_len, main_len, cache, stream)()
+
+
+def prepare_unpack_quant(shape, cache, res_len, main_len, kc, vc, first_slot=None, stream=None):
+    """As prepare_rope, for reskv_unpack_quant."""
+    import torch
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
+    pairs, n = shape.batch * shape.num_kv_heads, int(kc.shape[-2])
+    args = (ctypes.byref(shape), c, rl, ml, _tensor("first_slot", first_slot, torch.int32, pairs), n,
+            _tensor("kc", kc, _dtype(shape), pairs * n * shape.head_dim),
+            _tensor("vc", vc, _dtype(shape), pairs * n * shape.head_dim), _stream(stream))
+    return _prepared(lib().reskv_unpack_quant, args, (shape,))
+
+
+def reskv_unpack_quant(shape, cache, res_len, main_len, kc, vc, first_slot=None, stream=None):
+    """Values of the 4-bit cache into kc, vc [B, Hkv, n, d]: row i is slot first_slot + i (0 + i if None); rows
+    whose slot is not live are left as they were."""
+    prepare_unpack_quant(shape, cache, res_len, main_len, kc, vc, first_slot, stream)()
+
+
+def _turn(shape, rope, positions, n):
+    import torch
+    return (None if rope is None else ctypes.byref(rope),
+            _tensor("positions", positions, torch.int32, shape.batch * n))
+
+
+def prepare_append_kv_quant(shape, k_new, v_new, cache, res_len, main_len, rope=None, positions=None, n_tok=None,
+                            stream=None):
+    """As prepare_rope, for reskv_append_kv_quant."""
+    import torch
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
+    n = int(k_new.shape[2]) if k_new.dim() == 4 else 1
+    count = shape.batch * shape.num_kv_heads * n * shape.head_dim
+    args = (ctypes.byref(shape), *_turn(shape, rope, positions, n), n,
+            _tensor("n_tok", n_tok, torch.int32, shape.batch), _tensor("k_new", k_new, _dtype(shape), count),
+            _tensor("v_new", v_new, _dtype(shape), count), c, rl, ml, _stream(stream))
+    return _prepared(lib().reskv_append_kv_quant, args, (shape, rope))
+
+
+def reskv_append_kv_quant(shape, k_new, v_new, cache, res_len, main_len, rope=None, positions=None, n_tok=None,
+                          stream=None):
+    """Append k_new, v_new [B, Hkv, n, d] ([B, Hkv, d] for one token) to the 4-bit cache, keys rotated by
+    positions [B, n] where a plan is given; tokens from n_tok [B] on are padding."""
+    prepare_append_kv_quant(shape, k_new, v_new, cache, res_len, main_len, rope, positions, n_tok, stream)()
+
+
+def reskv_decode_quant_workspace_size(shape):
+    return lib().reskv_decode_quant_workspace_size(ctypes.byref(shape))
+
+
+def prepare_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, out, workspace, rope=None,
+                              positions=None, dbg_lse_main=None, dbg_lse_res=None, dbg_gate=None, k_new=None,
+                              v_new=None, stream=None):
+    """As prepare_rope, for reskv_decode_attn_quant."""
+    import torch
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
+    B, Hq, H, d = shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+    dt, f32 = _dtype(shape), torch.float32
+    args = (ctypes.byref(shape), ctypes.byref(gate), *_turn(shape, rope, positions, 1),
+            _tensor("q", q, dt, B * Hq * d), c, _tensor("logc", logc, f32, B * H * shape.res_cap), rl, ml,
+            _tensor("k_new", k_new, dt, B * H * d), _tensor("v_new", v_new, dt, B * H * d),
+            _tensor("out", out, f32, B * Hq * d), _tensor("dbg_lse_main", dbg_lse_main, f32, B * Hq),
+            _tensor("dbg_lse_res", dbg_lse_res, f32, B * Hq), _tensor("dbg_gate", dbg_gate, f32, B * Hq),
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    return _prepared(lib().reskv_decode_attn_quant, args, (shape, gate, rope))
+
+
+def reskv_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, out, workspace, rope=None, positions=None,
+                            dbg_lse_main=None, dbg_lse_res=None, dbg_gate=None, k_new=None, v_new=None, stream=None):
+    """One decode step over the 4-bit cache; with a plan, q and k_new are rotated by positions [B] on the way."""
+    prepare_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, out, workspace, rope, positions,
+                              dbg_lse_main, dbg_lse_res, dbg_gate, k_new, v_new, stream)()
 
 
 def status_string(status):

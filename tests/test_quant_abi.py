@@ -1,0 +1,159 @@
+"""Rotation plans, buffer sizes and refusals of the rotary positions and the 4-bit caches (no GPU needed)."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_29591_amd import reskv as rk
+from tests import quant_ref as ref
+
+P = 0x10000  # a pointer that no refused call follows
+
+
+def shape(**kw):
+    d = dict(batch=2, num_q_heads=8, num_kv_heads=2, head_dim=128, dtype="bf16", slot_cap=640, res_cap=64)
+    d.update(kw)
+    return rk.make_shape(**d)
+
+
+@pytest.mark.parametrize("rot", [16, 64, 96, 128])
+@pytest.mark.parametrize("kw", [
+    dict(), dict(theta=1e6), dict(scaling="linear", factor=4.0), dict(scaling="ntk", factor=8.0),
+    dict(scaling="llama3", theta=500000.0, factor=8.0, original_len=8192.0),
+    dict(scaling="llama3", factor=32.0, original_len=8192.0, low_freq_factor=2.0, high_freq_factor=3.0),
+    dict(scaling="yarn", factor=16.0, original_len=4096.0),
+    dict(scaling="yarn", factor=4.0, original_len=32768.0, beta_fast=64.0, beta_slow=2.0, theta=1e6),
+    dict(scaling="yarn", factor=4.0, original_len=10.0), dict(attn_scale=0.5), dict(scaling="linear", factor=1.0)])
+def test_plan_frequencies(rot, kw):
+    plan = rk.make_rope(rot, layout="interleaved", **kw)
+    f, scale = ref.frequencies(rot, **kw)
+    got = np.array(plan.freq[:rot // 2])
+    # both sides round a handful of operations, the power within an ulp or two: 16 * 2^-53 relative
+    assert (np.abs(got - f) <= 2.0 ** -49 * f).all()
+    assert abs(plan.attn_scale - scale) <= 2.0 ** -50 * scale
+    assert plan.rot_dim == rot and plan.layout == 1 and not any(plan.freq[rot // 2:])
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rot_dim=0), 2), (dict(rot_dim=24), 2), (dict(rot_dim=144), 2), (dict(rot_dim=64, layout=2), 1),
+    (dict(rot_dim=64, scaling=5), 1), (dict(rot_dim=64, scaling=-1), 1), (dict(rot_dim=64, theta=1.0), 1),
+    (dict(rot_dim=64, theta=float("nan")), 1), (dict(rot_dim=64, scaling="linear", factor=0.5), 1),
+    (dict(rot_dim=64, scaling="llama3", factor=8.0), 1), (dict(rot_dim=64, attn_scale=-1.0), 1),
+    (dict(rot_dim=64, scaling="llama3", factor=8.0, original_len=8192.0, low_freq_factor=4.0), 1),
+    (dict(rot_dim=64, scaling="yarn", factor=8.0, original_len=4096.0, beta_fast=1.0), 1),
+    (dict(rot_dim=64, attn_scale=float("inf")), 1)])
+def test_plan_refusals(kw, code):
+    with pytest.raises(rk.ReskvError) as e:
+        rk.make_rope(**kw)
+    assert e.value.status == code and rk.last_error()
+
+
+def test_sizes():
+    for d in (64, 128):
+        for C in (1, 63, 64, 65, 640):
+            assert rk.reskv_quant_cache_size(shape(head_dim=d, slot_cap=C)) == 2 * 2 * -(-C // 64) * 68 * d
+    assert rk.reskv_quant_cache_size(shape(head_dim=96)) == 0
+    assert rk.reskv_decode_quant_workspace_size(shape(head_dim=96)) == 0
+    assert rk.reskv_decode_quant_workspace_size(shape()) > 0
+    # 4.25 bits a number: codes, and one scale byte for 32 of them
+    assert rk.reskv_quant_cache_size(shape()) * 8 == 4.25 * 2 * 2 * 640 * 2 * 128
+
+
+def rope_call(s=None, plan=None, n=5, pos=P, q=P, qs=(5120, 640, 128), qo=P << 8, qos=(5120, 640, 128), k=None,
+              ks=None, ko=None, kos=None):
+    row = lambda x: None if x is None else ctypes.byref(rk.Rows(*x))  # noqa: E731
+    plan = None if plan == 0 else ctypes.byref(plan or rk.make_rope(128))
+    return rk.lib().reskv_rope(ctypes.byref(s or shape()), plan, n, pos, None, q, row(qs), qo, row(qos), k, row(ks), ko,
+                               row(kos), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(s=shape(head_dim=96)), 2), (dict(s=shape(dtype=7)), 2), (dict(plan=0), 1), (dict(pos=None), 1),
+    (dict(n=-1), 1), (dict(s=shape(head_dim=64)), 1),                    # the plan turns more than the row has
+    (dict(plan=rk.Rope(0, 0, 1.0)), 1), (dict(plan=rk.Rope(24, 0, 1.0)), 1), (dict(plan=rk.Rope(64, 2, 1.0)), 1),
+    (dict(plan=rk.Rope(64, 0, float("nan"))), 1),
+    (dict(q=None, qo=None), 1), (dict(q=None), 1), (dict(qo=None), 1), (dict(qs=None), 1), (dict(qos=None), 1),
+    (dict(q=P + 8), 1), (dict(qo=(P << 8) + 2), 1),                      # alignment
+    (dict(qs=(5120, 640, 132)), 1), (dict(qs=(5120, -640, 128)), 1), (dict(qos=(5120, 644, 128)), 1),
+    (dict(qs=(1 << 50, 640, 128)), 1),
+    (dict(qos=(5120, 0, 128)), 1), (dict(qos=(5120, 640, 120)), 1), (dict(qos=(5120, 512, 128)), 1),  # overlapping rows
+    (dict(qos=(2560, 640, 128)), 1),
+    (dict(qo=P + 512), 1), (dict(qo=P, qos=(5120, 128, 1024)), 1),       # over its own input
+    (dict(k=P << 12, ks=(1280, 640, 128)), 1),
+    (dict(k=P << 12, ks=(1280, 640, 128), ko=P << 13, kos=(1280, 0, 128)), 1)])
+def test_rope_refusals(kw, code):
+    assert rope_call(**kw) == code
+    assert rk.last_error()
+
+
+def test_rope_of_no_rows_is_fine():
+    assert rope_call(n=0) == 0
+
+
+def quant_call(name, **kw):
+    s = kw.pop("s", None) or shape()
+    plan = rk.make_rope(128)
+    turn = kw.pop("turn", (None, None))
+    turn = [None if turn[0] is None else ctypes.byref(rk.make_rope(turn[0])), turn[1]]
+    a = dict(kc=P, vc=P, rl=P, ml=P, cache=P, first=None, n=3, n_tok=None, q=P, logc=P, out=P, ws=P, bytes=1 << 40,
+             gate=ctypes.byref(rk.make_gate()))
+    a.update(kw)
+    del plan
+    L, ref_s = rk.lib(), ctypes.byref(s)
+    if name == "pack":
+        return L.reskv_pack_quant(ref_s, a["kc"], a["vc"], a["rl"], a["ml"], a["cache"], None)
+    if name == "unpack":
+        return L.reskv_unpack_quant(ref_s, a["cache"], a["rl"], a["ml"], a["first"], a["n"], a["kc"], a["vc"], None)
+    if name == "append":
+        return L.reskv_append_kv_quant(ref_s, *turn, a["n"], a["n_tok"], a["kc"], a["vc"], a["cache"], a["rl"],
+                                       a["ml"], None)
+    return L.reskv_decode_attn_quant(ref_s, a["gate"], *turn, a["q"], a["cache"], a["logc"], a["rl"], a["ml"],
+                                     a["kc"], a["vc"], a["out"], None, None, None, a["ws"], a["bytes"], None)
+
+
+@pytest.mark.parametrize("name,kw,code", [
+    (n, dict(s=shape(head_dim=96)), 2) for n in ("pack", "unpack", "append", "decode")] + [
+    (n, dict(s=shape(slot_cap=0)), 1) for n in ("pack", "unpack", "append", "decode")] + [
+    (n, {x: None}, 1) for n in ("pack", "unpack", "append") for x in ("kc", "vc", "rl", "ml", "cache")] + [
+    (n, {x: P + 4}, 1) for n in ("pack", "unpack", "append", "decode") for x in ("kc", "vc", "cache")] + [
+    ("decode", {x: None}, 1) for x in ("q", "cache", "logc", "rl", "ml", "out", "kc", "vc", "gate")] + [
+    ("unpack", dict(n=-1), 1), ("append", dict(n=-1), 1), ("decode", dict(q=P + 2), 1),
+    ("append", dict(turn=(128, None)), 1), ("append", dict(turn=(None, P)), 1),
+    ("append", dict(s=shape(head_dim=64), turn=(128, P)), 1),
+    ("decode", dict(turn=(128, None)), 1), ("decode", dict(turn=(None, P)), 1),
+    ("decode", dict(s=shape(head_dim=64), turn=(128, P)), 1),
+    ("decode", dict(ws=None), 3), ("decode", dict(bytes=0), 3),
+    ("decode", dict(gate=ctypes.byref(rk.make_gate(g_min=2.0))), 1)])
+def test_quant_refusals(name, kw, code):
+    assert quant_call(name, **kw) == code
+    assert rk.last_error()
+
+
+def test_nothing_to_do_is_fine():
+    assert quant_call("append", n=0) == 0 and quant_call("unpack", n=0) == 0
+
+
+def test_binding_refuses_wrong_tensors():
+    """Type, size, place and order of every tensor are checked before its pointer is taken."""
+    s, plan = shape(), rk.make_rope(128)
+    q = torch.zeros(2, 8, 5, 128, dtype=torch.bfloat16)
+    pos = torch.zeros(2, 5, dtype=torch.int32)
+    for bad in (dict(q=q.float(), q_out=q), dict(q=q[:, :7], q_out=q), dict(q=q, q_out=q[..., ::2]),
+                dict(q=q, q_out=q), dict(q=q[..., :64], q_out=q[..., :64])):  # the last but one: not on the GPU
+        with pytest.raises(ValueError):
+            rk.reskv_rope(s, plan, pos, **bad)
+    cache = torch.zeros(rk.reskv_quant_cache_size(s), dtype=torch.uint8)
+    lens, rows = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 2, 640, 128, dtype=torch.bfloat16)
+    for args in ((rows, rows, lens, lens, cache[:-1]), (rows, rows, lens, lens.long(), cache),
+                 (rows, rows, lens, lens, cache), (rows, rows, lens[:3], lens, cache)):
+        with pytest.raises(ValueError):
+            rk.reskv_pack_quant(s, *args)
+    with pytest.raises(ValueError):
+        rk.reskv_unpack_quant(s, cache, lens, lens, rows, rows)
+    with pytest.raises(ValueError):
+        rk.reskv_append_kv_quant(s, rows, rows, cache, lens, lens)
+    with pytest.raises(ValueError):
+        rk.reskv_decode_attn_quant(s, rk.make_gate(), q[:, :, 0].contiguous(), cache, torch.zeros(2, 2, 64), lens, lens,
+                                   torch.zeros(2, 8, 128), cache)

@@ -1,0 +1,179 @@
+"""Rotary positions on the GPU against the pair-by-pair rotation in 64 bits: layouts, parts of the head, scalings,
+positions up to the last 32-bit one, strides, padding, in place, streams and graphs."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_29591_amd import reskv as rk
+from tests import quant_ref as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+SCALINGS = {"none": {}, "linear": dict(factor=4.0), "ntk": dict(factor=8.0),
+            "llama3": dict(theta=500000.0, factor=8.0, original_len=8192.0),
+            "yarn": dict(factor=16.0, original_len=4096.0)}
+
+
+def rows(rng, dtype, *shape):
+    return torch.as_tensor(rng.normal(size=shape) * 2.0, dtype=torch.float32).to(DT[dtype]).cuda()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def check(x, got, pos, rot, dtype, live=None, fill=0.0, **kw):
+    want, atol = ref.rotate_atol(host(x), pos, rot, torch.finfo(DT[dtype]).eps, **kw)
+    if live is not None:
+        pad = np.arange(x.shape[2])[None, None, :, None] >= np.asarray(live)[:, None, None, None]
+        assert (host(got)[np.broadcast_to(pad, want.shape)] == fill).all()
+        want, atol = np.where(pad, fill, want), np.where(pad, 0.0, atol)
+    off = np.abs(host(got) - want) - atol
+    assert off.max() <= 0, f"{(off > 0).sum()} elements past the bound, worst by {off.max():.3g}"
+
+
+@pytest.mark.parametrize("scaling", list(SCALINGS))
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype,d,rot", [("bf16", 128, 128), ("bf16", 128, 48), ("bf16", 64, 64), ("f32", 128, 64),
+                                         ("f32", 64, 16)])
+def test_rotation(dtype, d, rot, layout, scaling):
+    rng = np.random.default_rng(rot + len(scaling))
+    B, Hq, H, n = 3, 6, 2, 37
+    q, k = rows(rng, dtype, B, Hq, n, d), rows(rng, dtype, B, H, n, d)
+    pos = rng.integers(0, 131072, size=(B, n)).astype(np.int32)
+    pos[0, :5] = [0, 1, -1, 2 ** 31 - 1, -2 ** 31]
+    kw = dict(layout=layout, scaling=scaling, **SCALINGS[scaling])
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    rk.reskv_rope(rk.make_shape(B, Hq, H, d, dtype, 1, 1), rk.make_rope(rot, **kw), torch.as_tensor(pos).cuda(), q=q,
+                  q_out=qo, k=k, k_out=ko)
+    check(q, qo, pos, rot, dtype, **kw)
+    check(k, ko, pos, rot, dtype, **kw)
+    assert torch.equal(qo[..., rot:], q[..., rot:])  # the rest of the head, bit for bit
+
+
+@pytest.mark.parametrize("B,Hq,H,n", [(1, 1, 1, 1), (1, 32, 8, 1), (33, 28, 4, 1), (1, 4, 4, 4097), (5, 16, 1, 131)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sizes(B, Hq, H, n, dtype):
+    rng = np.random.default_rng(n)
+    q, k = rows(rng, dtype, B, Hq, n, 128), rows(rng, dtype, B, H, n, 128)
+    pos = (rng.integers(0, 100000, size=(B, 1)) + np.arange(n)).astype(np.int32)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    rk.reskv_rope(rk.make_shape(B, Hq, H, 128, dtype, 1, 1), rk.make_rope(128), torch.as_tensor(pos).cuda(), q=q,
+                  q_out=qo, k=k, k_out=ko)
+    check(q, qo, pos, 128, dtype)
+    check(k, ko, pos, 128, dtype)
+
+
+def test_padding_is_left_as_it_was():
+    rng = np.random.default_rng(5)
+    B, n = 6, 70
+    q = rows(rng, "bf16", B, 4, n, 64)
+    n_tok = np.array([0, 1, 69, 70, 75, -3], np.int32)
+    out = torch.full_like(q, 7.0)
+    pos = rng.integers(0, 9999, size=(B, n)).astype(np.int32)
+    rk.reskv_rope(rk.make_shape(B, 4, 2, 64, "bf16", 1, 1), rk.make_rope(32), torch.as_tensor(pos).cuda(), q=q,
+                  q_out=out, n_tok=torch.as_tensor(n_tok).cuda())
+    check(q, out, pos, 32, "bf16", live=n_tok, fill=7.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_strides_and_in_place(dtype, layout):
+    """Queries and keys as parts of a fused projection [B, n, (Hq + 2 H) d], into head-major tensors and in place."""
+    rng = np.random.default_rng(6)
+    B, n, Hq, H, d = 2, 45, 8, 2, 128
+    fused = rows(rng, dtype, B, n, (Hq + 2 * H) * d)
+    before = fused.clone()
+    x = fused.view(B, n, Hq + 2 * H, d).transpose(1, 2)
+    q, k = x[:, :Hq], x[:, Hq:Hq + H]
+    pos = torch.as_tensor(rng.integers(0, 5000, size=(B, n)).astype(np.int32)).cuda()
+    shape, rope = rk.make_shape(B, Hq, H, d, dtype, 1, 1), rk.make_rope(96, layout=layout)
+    S = n + 19  # rows of a larger prefill tensor
+    qo = torch.full((B, Hq, S, d), 3.0, dtype=DT[dtype], device="cuda")
+    ko = torch.full((B, H, S, d), 3.0, dtype=DT[dtype], device="cuda")
+    rk.reskv_rope(shape, rope, pos, q=q, q_out=qo[:, :, 4:4 + n], k=k, k_out=ko[:, :, 4:4 + n])
+    assert torch.equal(fused, before)
+    check(q, qo[:, :, 4:4 + n], pos.cpu().numpy(), 96, dtype, layout=layout)
+    check(k, ko[:, :, 4:4 + n], pos.cpu().numpy(), 96, dtype, layout=layout)
+    for o in (qo, ko):
+        assert (o[:, :, :4] == 3.0).all() and (o[:, :, 4 + n:] == 3.0).all()
+    rk.reskv_rope(shape, rope, pos, q=q, q_out=q, k=k, k_out=k)
+    assert torch.equal(q, qo[:, :, 4:4 + n]) and torch.equal(k, ko[:, :, 4:4 + n])
+    assert torch.equal(fused[..., (Hq + H) * d:], before[..., (Hq + H) * d:])  # values untouched
+
+
+def test_broadcast_input_and_single_operand():
+    rng = np.random.default_rng(7)
+    k = rows(rng, "bf16", 1, 1, 9, 64).expand(3, 2, 9, 64)
+    out = torch.zeros(3, 2, 9, 64, dtype=torch.bfloat16, device="cuda")
+    pos = rng.integers(0, 5000, size=(3, 9)).astype(np.int32)
+    rk.reskv_rope(rk.make_shape(3, 8, 2, 64, "bf16", 1, 1), rk.make_rope(64), torch.as_tensor(pos).cuda(), k=k,
+                  k_out=out)
+    check(k, out, pos, 64, "bf16")
+
+
+def test_turning_back():
+    """Negative positions undo positive ones: two roundings of half a step, the second on rows of the same length."""
+    rng = np.random.default_rng(8)
+    x = rows(rng, "f32", 2, 3, 50, 128)
+    pos = torch.as_tensor(rng.integers(0, 100000, size=(2, 50)).astype(np.int32)).cuda()
+    shape, rope = rk.make_shape(2, 3, 1, 128, "f32", 1, 1), rk.make_rope(128, scaling="linear", factor=2.0)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    rk.reskv_rope(shape, rope, pos, q=x, q_out=y)
+    rk.reskv_rope(shape, rope, -pos, q=y, q_out=z)
+    pair = x.abs() + x.abs().roll(64, -1)
+    # each rounding is off by 2^-24 of a number within the pair's length; the first error is turned with its pair
+    assert ((z - x).abs() <= 3.5 * 2.0 ** -24 * pair).all()
+
+
+def test_infinities_stay_in_their_pair():
+    x = torch.ones(1, 1, 1, 128, device="cuda")
+    x[..., 3], x[..., 100] = float("inf"), float("nan")
+    y = torch.zeros_like(x)
+    rk.reskv_rope(rk.make_shape(1, 1, 1, 128, "f32", 1, 1), rk.make_rope(64), torch.full((1, 1), 9, dtype=torch.int32,
+                  device="cuda"), q=x, q_out=y)
+    bad = ~torch.isfinite(y[0, 0, 0])
+    assert bad.nonzero().flatten().tolist() == [3, 35, 100]
+
+
+def test_graph_replays_and_streams():
+    rng = np.random.default_rng(9)
+    B, Hq, H, n = 4, 8, 2, 3
+    shape, rope = rk.make_shape(B, Hq, H, 128, "bf16", 1, 1), rk.make_rope(128, scaling="yarn", factor=4.0,
+                                                                           original_len=4096.0)
+    q, k = rows(rng, "bf16", B, Hq, n, 128), rows(rng, "bf16", B, H, n, 128)
+    pos = torch.zeros(B, n, dtype=torch.int32, device="cuda")
+    qo, ko, qe, ke = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(q), torch.zeros_like(k)
+    rk.reskv_rope(shape, rope, pos, q=q, q_out=qe, k=k, k_out=ke)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rk.reskv_rope(shape, rope, pos, q=q, q_out=qo, k=k, k_out=ko)
+    for step in range(4):
+        pos.copy_(torch.as_tensor(rng.integers(0, 60000, size=(B, n)), dtype=torch.int32))
+        q.copy_(rows(rng, "bf16", B, Hq, n, 128))
+        torch.cuda.synchronize()
+        g.replay()
+        rk.reskv_rope(shape, rope, pos, q=q, q_out=qe, k=k, k_out=ke)
+        torch.cuda.synchronize()
+        assert torch.equal(qo, qe) and torch.equal(ko, ke), step
+    side = torch.cuda.Stream()
+    qs = torch.zeros_like(q)
+    side.wait_stream(torch.cuda.current_stream())
+    rk.reskv_rope(shape, rope, pos, q=q, q_out=qs, stream=side)
+    side.synchronize()
+    assert torch.equal(qs, qe)
+
+
+def test_rows_past_32_bit_offsets():
+    """A row whose element offset passes 2^31: the last head of a strided view of one large buffer."""
+    d, stride = 64, (1 << 30) + 64
+    buf = torch.zeros(2 * stride + d, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (1, 3, 1, d), (0, stride, 0, 1))
+    rng = np.random.default_rng(10)
+    x.copy_(rows(rng, "bf16", 1, 3, 1, d))
+    before = x.clone()
+    pos = torch.full((1, 1), 77, dtype=torch.int32, device="cuda")
+    rk.reskv_rope(rk.make_shape(1, 3, 1, d, "bf16", 1, 1), rk.make_rope(d), pos, q=x, q_out=x)
+    check(before, x.clone(), pos.cpu().numpy(), d, "bf16")
