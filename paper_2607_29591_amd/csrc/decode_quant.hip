@@ -1,10 +1,11 @@
 // Shared-softmax residual decode (Sec. 5.4; Sec. 5.5.2 gate; App. D, Algorithm 2)
 // over a cache held in 4 bits.
 //
-// One block of 8 waves per (b, kv head); a wave takes blocks of 64 slots (the
-// cache's own blocks) and keeps a running maximum, sum and output per query head
-// for the residual slots, then for the main slots; the waves' states are merged
-// in LDS, where the gate joins the two kinds. With hd = lane % 16, g = lane / 16:
+// One block of 8 waves per (b, kv head), or several where few heads have long
+// caches; a wave takes blocks of 64 slots (the cache's own blocks) and keeps a
+// running maximum, sum and output per query head for the residual slots, then for
+// the main slots; the waves' states are merged in LDS, where the gate joins the
+// two kinds, or in a second launch over the blocks' records. With hd = lane % 16, g = lane / 16:
 //   * logits S^T = K Q^T per 16-slot tile t: lane (hd, g) loads D / 4 elements
 //     of key row 16t + hd (16 bytes at D = 128), all of one scale, which the
 //     conversion applies: every code times its scale is a bf16 number, so the
@@ -30,6 +31,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kUnit = 64;  // slots of a cache block
 constexpr int kTiles = kUnit / 16;
+constexpr int kMaxParts = 64;  // blocks a head is split over
 
 struct QuantDecodeArgs {
   reskv_rope_t rope;
@@ -46,7 +48,10 @@ struct QuantDecodeArgs {
   float* dbg_lse_main;
   float* dbg_lse_res;
   float* dbg_gate;
+  float* rec_ml;   // split: [BH][P][2 kinds][GP][2] (maximum in base 2, sum)
+  float* rec_acc;  // split: [BH][P][2 kinds][GP][D], written for kinds with slots
   int Hq, Hkv, G, C, Rcap, NB;
+  int P, W;        // blocks of a head and cache blocks of each (unsplit: 1, NB)
   float qk_scale;   // log2(e) / sqrt(d)
   float beta_log2;  // beta * log2(e)
   float tau_scalar, alpha, g_min;
@@ -240,7 +245,8 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const
     }
   sum = rows4_sum(sum);
   st.l = fmaf(st.l, alpha, sum);
-  st.m = m_new;
+  // logits that are all NaN leave no maximum: 0 in its place keeps their sum in the merges
+  st.m = m_new == kNegInf && sum != 0.f ? 0.f : m_new;
 #pragma unroll
   for (int e = 0; e < State<D>::kE; ++e)
 #pragma unroll
@@ -262,11 +268,42 @@ __device__ __forceinline__ void store_state(const State<D>& st, float (*acc)[D],
   }
 }
 
-template <typename T, int D, int GP>
-__global__ __launch_bounds__(kThreads) void decode_quant_head(QuantDecodeArgs a) {
+// The gate joins the two kinds of one (query head, column): maxima, sums and
+// unnormalised outputs in, the output out.
+struct Joined {
+  float gate, fM, fR, inv;  // factors on the main and residual sums, 1 / denominator
+};
+__device__ __forceinline__ Joined join(const QuantDecodeArgs& a, int qh, float mM, float lM, float mR, float lR) {
+  const float tau = a.tau ? a.tau[qh] : a.tau_scalar;
+  // p_max = 1 / l_main (the largest term is exactly 1), then the gate
+  const float pmax = lM > 0.f ? 1.f / lM : 1.f;
+  Joined j;
+  j.gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
+  const float lg = j.gate > 0.f ? log2f(j.gate) : kNegInf;
+  const float mRg = (mR == kNegInf || lg == kNegInf) ? kNegInf : mR + lg;
+  const float M = fmaxf(mM, mRg);
+  j.fM = mM != kNegInf ? exp2f(mM - M) : 0.f;
+  j.fR = mRg != kNegInf ? exp2f(mRg - M) : 0.f;
+  const float den = lM * j.fM + lR * j.fR;
+  j.inv = den != 0.f ? 1.f / den : 0.f;  // NaN stays NaN
+  return j;
+}
+__device__ __forceinline__ void write_stats(const QuantDecodeArgs& a, int qh, float mM, float lM, float mR, float lR,
+                                            float gate) {
+  if (a.dbg_lse_main) a.dbg_lse_main[qh] = lM != 0.f ? (mM + log2f(lM)) * kLn2 : kNegInf;
+  if (a.dbg_lse_res) a.dbg_lse_res[qh] = lR != 0.f ? (mR + log2f(lR)) * kLn2 : kNegInf;
+  if (a.dbg_gate) a.dbg_gate[qh] = gate;
+}
+
+// Block p of P of a (b, kv head): its cache blocks [p W, (p + 1) W). kSplit: the
+// merged states of both kinds go to records, which decode_quant_combine joins;
+// else this block has the whole head and finishes it.
+template <typename T, int D, int GP, bool kSplit>
+__global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs a) {
   using Q = QuantBlock<D>;
   constexpr int NP = sizeof(T) == 2 ? 1 : 3;
-  const int bh = blockIdx.x, b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const int bh = kSplit ? blockIdx.x / a.P : blockIdx.x, part = kSplit ? blockIdx.x % a.P : 0;
+  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int hd = lane & 15, g = lane >> 4;
   uint8_t* cache = a.cache + (size_t)bh * a.NB * Q::kBytes;
@@ -283,11 +320,21 @@ __global__ __launch_bounds__(kThreads) void decode_quant_head(QuantDecodeArgs a)
   const bool app = a.k_new != nullptr && r + n < a.C;
   const int app_slot = r + n;
   if (app) n += 1;
+  const int total = r + n;
+  const int begin = part * a.W, end = min(begin + a.W, (total + kUnit - 1) / kUnit);
+  if (kSplit && begin >= end) {  // no live slot here: records without weight
+    for (int i = tid; i < 2 * GP; i += kThreads) {
+      float* ml = a.rec_ml + (((size_t)bh * a.P + part) * 2 * GP + i) * 2;
+      ml[0] = kNegInf;
+      ml[1] = 0.f;
+    }
+    return;
+  }
   const int rot = a.positions ? a.rope.rot_dim : 0;
   if (tid < rot / 2) s_cs[tid] = turn(a.rope.freq[tid], a.positions[b], a.rope.attn_scale);
   __syncthreads();
   // this step's token into the cache (wave 0 the key, wave 1 the value)
-  if (app && wave < 2) {
+  if (app && wave < 2 && app_slot / kUnit >= begin && app_slot / kUnit < end) {
     const T* src = static_cast<const T*>(wave ? a.v_new : a.k_new) + (size_t)bh * D;
     const int l = min(lane, D / 2 - 1), rk = wave ? 0 : rot;
     store_row_quant<D>(cache + (size_t)(app_slot / kUnit) * Q::kBytes, app_slot % kUnit, wave == 1,
@@ -316,39 +363,36 @@ __global__ __launch_bounds__(kThreads) void decode_quant_head(QuantDecodeArgs a)
     for (int i = 0; i < D / 32; ++i)
       q[p].s[i] = hd < GP ? *reinterpret_cast<const uint4*>(&s_q[p][hd][g * (D / 4) + 8 * i]) : make_uint4(0, 0, 0, 0);
 
-  // Work list: the blocks that hold residual slots, then those that hold main
-  // slots (the block of slot r, if both, in both parts), dealt to the waves in
-  // turn, so that a wave meets its residual blocks first.
-  const int total = r + n;
-  const int UR = (r + kUnit - 1) / kUnit, first_main = r / kUnit;
-  const int U = UR + (n > 0 ? (total + kUnit - 1) / kUnit - first_main : 0);
+  // The waves take the cache blocks in turn; residual slots come first, and the
+  // block that holds slot r has a part of each kind.
   State<D> st;
   st.reset();
   bool in_res = true;
-  for (int p = wave; p < U; p += kWaves) {
-    const bool is_res = p < UR;
-    if (!is_res && in_res) {
-      store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
-      st.reset();
-      in_res = false;
-    }
-    const int blk = is_res ? p : first_main + p - UR;
-    const int lo = is_res ? 0 : r - blk * kUnit, hi = (is_res ? r : total) - blk * kUnit;
+  for (int blk = begin + wave; blk < end; blk += kWaves) {
     Unit<D> u;
     u.load(cache + (size_t)blk * Q::kBytes, hd, g);
+    const int s0 = blk * kUnit;
     float lc[kTiles][4] = {};
-    if (is_res) {
+    if (s0 < r) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = 16 * t + 4 * g + i;
-          lc[t][i] = j < hi ? logc[blk * kUnit + j] : 0.f;
+          const int j = s0 + 16 * t + 4 * g + i;
+          lc[t][i] = j < r ? logc[j] : 0.f;
         }
     }
     float s[kTiles][4];
     unit_logits<D, NP>(u, q, a.qk_scale, s);
-    softmax_pv<D>(st, u, s, lc, lo, hi, is_res, a.beta_log2, g);
+    if (s0 < r) softmax_pv<D>(st, u, s, lc, 0, r - s0, true, a.beta_log2, g);
+    if (s0 + kUnit > r && s0 < total) {
+      if (in_res) {
+        store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
+        st.reset();
+        in_res = false;
+      }
+      softmax_pv<D>(st, u, s, lc, r - s0, total - s0, false, 0.f, g);
+    }
   }
   if (in_res) {
     store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
@@ -373,42 +417,111 @@ __global__ __launch_bounds__(kThreads) void decode_quant_head(QuantDecodeArgs a)
       }
     }
   };
-  for (int i = tid; i < a.G * D; i += kThreads) {
-    const int h = i / D, d = i % D;
-    float mR, lR, oR, mM, lM, oM;
-    merge(0, h, d, mR, lR, oR);
-    merge(1, h, d, mM, lM, oM);
-    const int qh = b * a.Hq + kvh * a.G + h;
-    const float tau = a.tau ? a.tau[qh] : a.tau_scalar;
-    // p_max = 1 / l_main (the largest term is exactly 1), then the gate
-    const float pmax = lM > 0.f ? 1.f / lM : 1.f;
-    const float gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
-    const float lg = gate > 0.f ? log2f(gate) : kNegInf;
-    const float mRg = (mR == kNegInf || lg == kNegInf) ? kNegInf : mR + lg;
-    const float M = fmaxf(mM, mRg);
-    const float fM = mM != kNegInf ? exp2f(mM - M) : 0.f;
-    const float fR = mRg != kNegInf ? exp2f(mRg - M) : 0.f;
-    const float den = lM * fM + lR * fR;
-    const float num = oM * fM + oR * fR;
-    a.out[(size_t)qh * D + d] = den != 0.f ? num / den : 0.f;  // NaN stays NaN
-    if (d == 0) {
-      if (a.dbg_lse_main) a.dbg_lse_main[qh] = lM != 0.f ? (mM + log2f(lM)) * kLn2 : kNegInf;
-      if (a.dbg_lse_res) a.dbg_lse_res[qh] = lR != 0.f ? (mR + log2f(lR)) * kLn2 : kNegInf;
-      if (a.dbg_gate) a.dbg_gate[qh] = gate;
+  if constexpr (kSplit) {
+    for (int i = tid; i < 2 * GP * D; i += kThreads) {
+      const int kind = i / (GP * D), h = i / D % GP, d = i % D;
+      float M, l, o;
+      merge(kind, h, d, M, l, o);
+      const size_t row = ((size_t)bh * a.P + part) * 2 * GP + kind * GP + h;
+      if (M != kNegInf) a.rec_acc[row * D + d] = o;
+      if (d == 0) {
+        a.rec_ml[row * 2] = M;
+        a.rec_ml[row * 2 + 1] = l;
+      }
+    }
+  } else {
+    for (int i = tid; i < a.G * D; i += kThreads) {
+      const int h = i / D, d = i % D;
+      float mR, lR, oR, mM, lM, oM;
+      merge(0, h, d, mR, lR, oR);
+      merge(1, h, d, mM, lM, oM);
+      const int qh = b * a.Hq + kvh * a.G + h;
+      const Joined j = join(a, qh, mM, lM, mR, lR);
+      a.out[(size_t)qh * D + d] = (oM * j.fM + oR * j.fR) * j.inv;
+      if (d == 0) write_stats(a, qh, mM, lM, mR, lR, j.gate);
+    }
+    if (app && tid == 0) a.main_len[bh] = n;
+  }
+}
+
+// Join the records of one query head: one block of D threads, thread d a column.
+// Every record has its maximum and sum (those without slots -inf and 0), so the
+// cache lengths are not read, and main_len advances here: by the block of the
+// group's first head, which alone reads it.
+template <int D, int GP>
+__global__ __launch_bounds__(D) void decode_quant_combine(QuantDecodeArgs a) {
+  const int bh = blockIdx.x / a.G, h = blockIdx.x % a.G, b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const int d = threadIdx.x, lane = d & 63;
+  __shared__ float s_w[2 * kMaxParts];
+  const size_t row0 = (size_t)bh * a.P * 2 * GP + h;  // record i = 2 p + kind is row i GP further
+  const float2* ml = reinterpret_cast<const float2*>(a.rec_ml) + row0;
+  constexpr int kPer = 2 * kMaxParts / 64;
+  const bool is_main = lane & 1;  // a lane's records are all of one kind
+  float2 e[kPer];
+  float own = kNegInf;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = lane + 64 * k;
+    e[k] = i < 2 * a.P ? ml[(size_t)i * GP] : make_float2(kNegInf, 0.f);
+    own = fmaxf(own, e[k].x);
+  }
+#pragma unroll
+  for (int x = 2; x < 64; x <<= 1) own = wave_xor_max(own, x);
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+    if (e[k].x != kNegInf) sum = fmaf(e[k].y, exp2f(e[k].x - own), sum);
+#pragma unroll
+  for (int x = 2; x < 64; x <<= 1) sum = wave_xor_add(sum, x);
+  const float mR = __shfl(own, 0, 64), mM = __shfl(own, 1, 64), lR = __shfl(sum, 0, 64), lM = __shfl(sum, 1, 64);
+  const int qh = b * a.Hq + kvh * a.G + h;
+  const Joined j = join(a, qh, mM, lM, mR, lR);
+  if (d < 64) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)  // -1: a record without slots, whose outputs were not written
+      s_w[lane + 64 * k] = e[k].x != kNegInf ? exp2f(e[k].x - own) * (is_main ? j.fM : j.fR) * j.inv : -1.f;
+  }
+  __syncthreads();
+  const float* acc = a.rec_acc + row0 * D + d;
+  float o = 0.f;
+  for (int i0 = 0; i0 < 2 * a.P; i0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      v[k] = i0 + k < 2 * a.P && !(s_w[i0 + k] < 0.f) ? acc[(size_t)(i0 + k) * GP * D] : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k < 2 * a.P && !(s_w[i0 + k] < 0.f)) o = fmaf(s_w[i0 + k], v[k], o);
+  }
+  a.out[(size_t)qh * D + d] = o;
+  if (d == 0) {
+    write_stats(a, qh, mM, lM, mR, lR, j.gate);
+    if (h == 0 && a.k_new) {
+      int r, n;
+      cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
+      if (r + n < a.C) a.main_len[bh] = n + 1;
     }
   }
-  if (app && tid == 0) a.main_len[bh] = n;
+}
+
+template <typename T, int D, int GP>
+void launch_kernels(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStream_t stream) {
+  if (pl.P == 1) {
+    hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, false>), dim3(pl.BH), dim3(kThreads), 0, stream, da);
+    return;
+  }
+  hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.BH * pl.P), dim3(kThreads), 0, stream, da);
+  hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(pl.BH * da.G), dim3(D), 0, stream, da);
 }
 
 template <typename T, int D>
 hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStream_t stream) {
-  const dim3 grid(pl.BH), block(kThreads);
   switch (pl.GP) {
-    case 1: hipLaunchKernelGGL((decode_quant_head<T, D, 1>), grid, block, 0, stream, da); break;
-    case 2: hipLaunchKernelGGL((decode_quant_head<T, D, 2>), grid, block, 0, stream, da); break;
-    case 4: hipLaunchKernelGGL((decode_quant_head<T, D, 4>), grid, block, 0, stream, da); break;
-    case 8: hipLaunchKernelGGL((decode_quant_head<T, D, 8>), grid, block, 0, stream, da); break;
-    default: hipLaunchKernelGGL((decode_quant_head<T, D, 16>), grid, block, 0, stream, da); break;
+    case 1: launch_kernels<T, D, 1>(pl, da, stream); break;
+    case 2: launch_kernels<T, D, 2>(pl, da, stream); break;
+    case 4: launch_kernels<T, D, 4>(pl, da, stream); break;
+    case 8: launch_kernels<T, D, 8>(pl, da, stream); break;
+    default: launch_kernels<T, D, 16>(pl, da, stream); break;
   }
   return hipGetLastError();
 }
@@ -420,7 +533,18 @@ QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   p.BH = s.batch * s.num_kv_heads;
   const int G = s.num_q_heads / s.num_kv_heads;
   p.GP = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : G <= 8 ? 8 : 16;
-  p.bytes = 256;
+  const int NB = (s.slot_cap + kUnit - 1) / kUnit;
+  p.P = 1;
+  p.W = NB;
+  if (p.BH < 256 && NB > 2 * kWaves) {
+    const int want = 256 / p.BH < kMaxParts ? 256 / p.BH : kMaxParts;
+    p.W = (NB + want - 1) / want;
+    p.W = (p.W + kWaves - 1) / kWaves * kWaves;
+    p.P = (NB + p.W - 1) / p.W;
+  }
+  const size_t rows = p.P > 1 ? (size_t)p.BH * p.P * 2 * p.GP : 0;
+  p.acc_off = align_up(rows * 2 * sizeof(float), 256);
+  p.bytes = align_up(p.acc_off + rows * s.head_dim * sizeof(float), 256) + 256;  // never 0
   return p;
 }
 
@@ -429,13 +553,15 @@ hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, co
                                const float* logc, const int32_t* res_len, int32_t* main_len, const void* k_new,
                                const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
                                float* dbg_gate, void* workspace, hipStream_t stream) {
-  (void)workspace;
   QuantDecodeArgs da{};
   if (rope) da.rope = *rope;
   da.positions = rope ? positions : nullptr;
   da.q = q; da.cache = (uint8_t*)cache; da.logc = logc;
   da.res_len = res_len; da.main_len = main_len; da.k_new = k_new; da.v_new = v_new;
   da.tau = g.tau; da.out = out;
+  da.rec_ml = static_cast<float*>(workspace);
+  da.rec_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.acc_off);
+  da.P = pl.P; da.W = pl.W;
   da.dbg_lse_main = dbg_lse_main; da.dbg_lse_res = dbg_lse_res; da.dbg_gate = dbg_gate;
   da.Hq = s.num_q_heads; da.Hkv = s.num_kv_heads; da.G = s.num_q_heads / s.num_kv_heads;
   da.C = s.slot_cap; da.Rcap = s.res_cap; da.NB = (s.slot_cap + kUnit - 1) / kUnit;

@@ -85,7 +85,8 @@ hipError_t launch_append_quant(const reskv_shape_t& s, const reskv_rope_t* rope,
 
 struct QuantDecodePlan {
   int BH, GP;
-  size_t bytes;
+  int P, W;  // blocks a (b, kv head) is split over, 64-slot cache blocks of each
+  size_t acc_off, bytes;
 };
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s);
 hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, const QuantDecodePlan& pl,

@@ -189,6 +189,10 @@ def test_nan_and_huge_keys_reach_the_output():
     rk.reskv_pack_quant(c.shape, kc, vc, c.res_len, c.main_len, c.cache)
     out = c.decode({})[0]
     assert torch.isnan(out[0, :2]).all()
+    c.main_len.clamp_(max=1)  # and where nothing but that key is left
+    c.logc_dev.fill_(-float("inf"))
+    assert torch.isnan(c.decode({})[0][0, :2]).all()
+    c.main_len.copy_(i32(c.n))
     c.q.mul_(1e-30)
     out = c.decode({})[0]
     want = torch.as_tensor(ref.quantize(host(vc))[0][0, 1, int(c.r[0, 1])]).cuda()
