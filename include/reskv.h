@@ -531,14 +531,16 @@ typedef struct {
   double attn_scale;    /* A; 0 takes the scaling's own (1, but for YARN) */
 } reskv_rope_params_t;
 
-typedef struct {        /* a plan, filled by reskv_rope_init; plain data */
+typedef struct {        /* a plan */
   int32_t rot_dim, layout;
   double attn_scale;
-  double freq[64];      /* radians a position, pairs [0, rot_dim / 2) */
+  const double* freq;   /* device [rot_dim / 2]: radians a position, by pair */
 } reskv_rope_t;
 
-/* Fill a rotation plan (host only; no GPU work). */
-reskv_status_t reskv_rope_init(const reskv_rope_params_t* params, reskv_rope_t* rope);
+/* Fill a rotation plan and its frequencies (host only; no GPU work). The caller
+ * copies freq_host [rot_dim / 2] to the device and sets rope->freq (NULL here). */
+reskv_status_t reskv_rope_init(const reskv_rope_params_t* params, reskv_rope_t* rope,
+                               double* freq_host);
 
 typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
   int64_t batch, head, row;  /* strides in elements; elements of a row adjoin */

@@ -248,8 +248,8 @@ reskv_status_t reskv_append_kv(const reskv_shape_t* shape, const void* k_new, co
 // Row accesses move 16 bytes.
 static bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-reskv_status_t reskv_rope_init(const reskv_rope_params_t* p, reskv_rope_t* rope) {
-  if (!p || !rope) return fail(RESKV_ERR_INVALID_ARG, "params or rope is NULL");
+reskv_status_t reskv_rope_init(const reskv_rope_params_t* p, reskv_rope_t* rope, double* freq_host) {
+  if (!p || !rope || !freq_host) return fail(RESKV_ERR_INVALID_ARG, "params, rope or freq_host is NULL");
   if (p->rot_dim < 16 || p->rot_dim > 128 || p->rot_dim % 16 != 0)
     return fail(RESKV_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [16, 128]", p->rot_dim);
   if (p->layout != RESKV_ROPE_HALF && p->layout != RESKV_ROPE_INTERLEAVED)
@@ -270,20 +270,19 @@ reskv_status_t reskv_rope_init(const reskv_rope_params_t* p, reskv_rope_t* rope)
                 p->beta_slow);
   if (!(p->attn_scale >= 0.0) || !isfinite(p->attn_scale))
     return fail(RESKV_ERR_INVALID_ARG, "attn_scale %g must be >= 0", p->attn_scale);
-  make_rope(*p, rope);
+  make_rope(*p, rope, freq_host);
   return ok();
 }
 
-// A plan as reskv_rope_init leaves it, for rows of `shape`.
+// A plan of reskv_rope_init with its frequencies on the device, for rows of `shape`.
 static reskv_status_t check_rope(const reskv_shape_t* s, const reskv_rope_t* rope) {
   if (rope->rot_dim < 16 || rope->rot_dim % 16 != 0 || rope->rot_dim > s->head_dim)
     return fail(RESKV_ERR_INVALID_ARG, "rot_dim %d of the plan is not a multiple of 16 in [16, head_dim = %d]",
                 rope->rot_dim, s->head_dim);
   if (rope->layout != RESKV_ROPE_HALF && rope->layout != RESKV_ROPE_INTERLEAVED)
     return fail(RESKV_ERR_INVALID_ARG, "layout %d of the plan is neither HALF (0) nor INTERLEAVED (1)", rope->layout);
-  bool fine = isfinite(rope->attn_scale);
-  for (int i = 0; i < rope->rot_dim / 2; ++i) fine = fine && isfinite(rope->freq[i]);
-  if (!fine) return fail(RESKV_ERR_INVALID_ARG, "the plan holds numbers that are not finite");
+  if (!isfinite(rope->attn_scale)) return fail(RESKV_ERR_INVALID_ARG, "attn_scale of the plan must be finite");
+  if (!rope->freq) return fail(RESKV_ERR_INVALID_ARG, "the plan has no frequencies on the device");
   return RESKV_OK;
 }
 
@@ -426,6 +425,7 @@ reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_g
     return fail(RESKV_ERR_INVALID_ARG, "k_new and v_new must both be given or both be NULL");
   if (!aligned(q) || !aligned(cache) || !aligned(k_new) || !aligned(v_new))
     return fail(RESKV_ERR_INVALID_ARG, "q, k_new, v_new and cache must be aligned to 16 bytes");
+  if (shape->batch > 65535) return fail(RESKV_ERR_UNSUPPORTED, "batch %d above 65535", shape->batch);
   const QuantDecodePlan plan = make_quant_decode_plan(*shape);
   if (!workspace || workspace_bytes < plan.bytes)
     return fail(RESKV_ERR_WORKSPACE, "decode needs %zu workspace bytes, got %zu", plan.bytes,

@@ -50,7 +50,7 @@ struct QuantDecodeArgs {
   float* dbg_gate;
   float* rec_ml;   // split: [BH][P][2 kinds][GP][2] (maximum in base 2, sum)
   float* rec_acc;  // split: [BH][P][2 kinds][GP][D], written for kinds with slots
-  int Hq, Hkv, G, C, Rcap, NB;
+  int G, C, Rcap, NB;
   int P, W;        // blocks of a head and cache blocks of each (unsplit: 1, NB)
   float qk_scale;   // log2(e) / sqrt(d)
   float beta_log2;  // beta * log2(e)
@@ -83,7 +83,10 @@ struct Unit {
   uint32_t ks;             // their scales, byte t
   Words<D / 8> v[kTiles];  // value codes of piece hd, rows 16T + 4g + u
   Words<16> vs;            // their scales, word T, byte u
-  __device__ __forceinline__ void load(const uint8_t* block, int hd, int g) {
+  float lc;                // log-count of slot `lane` (of an entry; else unused)
+  __device__ __forceinline__ void load(const uint8_t* cache, int blk, const float* logc, int Rcap, int lane) {
+    const uint8_t* block = cache + (size_t)blk * QuantBlock<D>::kBytes;
+    const int hd = lane & 15, g = lane >> 4;
     using Q = QuantBlock<D>;
     constexpr int kLanes = 4 / Q::kGroups;  // lane groups of one key scale
 #pragma unroll
@@ -92,6 +95,7 @@ struct Unit {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) v[t].load(block + Q::v_code(16 * t + 4 * g, hd));
     vs.load(block + Q::v_scale(4 * g, hd * Q::kPiece / 32));
+    lc = logc[min(blk * kUnit + lane, Rcap - 1)];
   }
 };
 
@@ -114,8 +118,7 @@ __device__ __forceinline__ uint4 eight(uint32_t codes, float scale) {
 }
 
 template <int D, int NP>
-__device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[NP], float qk_scale,
-                                            float (&s)[kTiles][4]) {
+__device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[NP], float (&s)[kTiles][4]) {
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const float scale = t == 0 ? byte_scale<0>(u.ks) : t == 1 ? byte_scale<1>(u.ks)
@@ -129,7 +132,7 @@ __device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16x8(q[p].s[i]), c, 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[t][i] = c[i] * qk_scale;
+    for (int i = 0; i < 4; ++i) s[t][i] = c[i];
   }
 }
 
@@ -153,10 +156,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
 }
 
+// Up to 8 query heads take half of the 16 columns of a matrix instruction: the
+// other half holds the same heads, with the low parts of their probabilities
+// (one product where more heads need two).
+template <int GP>
+constexpr bool kPaired = GP <= 8;
+
 // O^T += V^T P^T for the unit; rows without weight must hold finite numbers.
-template <int D>
+template <int D, int GP>
 __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const float (&vs)[kTiles][4],
-                                        const float (&p)[kTiles][4]) {
+                                        const float (&p)[kTiles][4], int hd) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t bh[4], bl[4];
@@ -165,6 +174,7 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
       const float pa = p[2 * h + w / 2][2 * (w % 2)], pb = p[2 * h + w / 2][2 * (w % 2) + 1];
       bh[w] = pack_bf16(pa, pb);
       bl[w] = pack_bf16(pa - bf16_lo(bh[w]), pb - bf16_hi(bh[w]));
+      if (kPaired<GP> && hd >= 8) bh[w] = bl[w];
     }
     const bf16x8_t Bh = as_bf16x8(make_uint4(bh[0], bh[1], bh[2], bh[3]));
     const bf16x8_t Bl = as_bf16x8(make_uint4(bl[0], bl[1], bl[2], bl[3]));
@@ -178,7 +188,7 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
         for (int w = 0; w < 4; ++w) a[w] = __builtin_amdgcn_perm(x[2 * w + 1], x[2 * w], sel);
         const bf16x8_t A = as_bf16x8(make_uint4(a[0], a[1], a[2], a[3]));
         st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bh, st.acc[e + o], 0, 0, 0);
-        st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bl, st.acc[e + o], 0, 0, 0);
+        if (!kPaired<GP>) st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bl, st.acc[e + o], 0, 0, 0);
       }
     };
     uint32_t x[8];
@@ -206,43 +216,61 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
   }
 }
 
-// Online softmax over the unit's slots [lo, hi) of one kind. Residual slots add
-// beta * log2 count; slots of no weight (outside, empty entries) get zero
-// probability and a zero scale, so whatever their codes say does not enter.
-template <int D>
+// Online softmax over the unit's slots [lo, hi) of one kind, from the logits'
+// products s. Residual slots add beta * log2 count; slots of no weight (outside,
+// empty entries) get zero probability and a zero scale, so whatever their codes
+// say does not enter. A unit full of main slots needs none of that.
+template <int D, int GP>
 __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const float (&s)[kTiles][4],
-                                           const float (&lc)[kTiles][4], int lo, int hi, bool is_res,
-                                           float beta_log2, int g) {
+                                           int lo, int hi, bool is_res, float qk_scale, float beta_log2, int hd,
+                                           int g) {
   float p[kTiles][4], vs[kTiles][4];
-  float top = kNegInf;
+  float top = kNegInf, m_new, mu;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     vs[t][0] = byte_scale<0>(u.vs.w[t]);
     vs[t][1] = byte_scale<1>(u.vs.w[t]);
     vs[t][2] = byte_scale<2>(u.vs.w[t]);
     vs[t][3] = byte_scale<3>(u.vs.w[t]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = 16 * t + 4 * g + i;
-      const bool live = j >= lo && j < hi && !(is_res && lc[t][i] == kNegInf);
-      const float v = is_res ? fmaf(beta_log2, lc[t][i], s[t][i]) : s[t][i];
-      p[t][i] = live ? v : kNegInf;
-      vs[t][i] = live ? vs[t][i] : 0.f;
-      top = fmaxf(top, p[t][i]);
-    }
   }
-  top = rows4_max(top);
-  const float m_new = fmaxf(st.m, top);
-  const float mu = m_new == kNegInf ? 0.f : m_new;
+  if (!is_res && lo <= 0 && hi >= kUnit) {  // wave-uniform
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+    m_new = fmaxf(st.m, rows4_max(top) * qk_scale);
+    mu = m_new == kNegInf ? 0.f : m_new;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(fmaf(s[t][i], qk_scale, -mu));
+  } else {
+    const float from = is_res ? u.lc : 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = 16 * t + 4 * g + i;
+        const float lc = __shfl(from, j, 64);
+        const bool live = j >= lo && j < hi && lc != kNegInf;
+        const float v = s[t][i] * qk_scale + beta_log2 * lc;
+        p[t][i] = live ? v : kNegInf;
+        vs[t][i] = live ? vs[t][i] : 0.f;
+        top = fmaxf(top, p[t][i]);
+      }
+    m_new = fmaxf(st.m, rows4_max(top));
+    mu = m_new == kNegInf ? 0.f : m_new;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(p[t][i] - mu);
+  }
   const float alpha = fast_exp2(st.m - mu);
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      p[t][i] = fast_exp2(p[t][i] - mu);
-      sum += p[t][i];
-    }
+    for (int i = 0; i < 4; ++i) sum += p[t][i];
   sum = rows4_sum(sum);
   st.l = fmaf(st.l, alpha, sum);
   // logits that are all NaN leave no maximum: 0 in its place keeps their sum in the merges
@@ -251,20 +279,29 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const
   for (int e = 0; e < State<D>::kE; ++e)
 #pragma unroll
     for (int i = 0; i < 4; ++i) st.acc[e][i] *= alpha;
-  pv_unit<D>(st, u, vs, p);
+  pv_unit<D, GP>(st, u, vs, p, hd);
 }
 
 template <int D, int GP>
-__device__ __forceinline__ void store_state(const State<D>& st, float (*acc)[D], float* m, float* l, int hd, int g) {
-  if (hd >= GP) return;
+__device__ __forceinline__ void store_state(State<D>& st, float (*acc)[D], float* m, float* l, int hd, int g) {
   constexpr int kE = D / 16;
+  if (kPaired<GP>) {  // the other half's part (row_ror:8)
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int e = 0; e < kE; ++e)
 #pragma unroll
-    for (int e = 0; e < kE; ++e) acc[hd][kE * (4 * g + i) + e] = st.acc[e][i];
-  if (g == 0) {
-    m[hd] = st.m;
-    l[hd] = st.l;
+      for (int i = 0; i < 4; ++i) st.acc[e][i] += dpp_move<0x128>(st.acc[e][i]);
+  }
+  if (hd < GP) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < kE; e += 4)
+        *reinterpret_cast<float4*>(&acc[hd][kE * (4 * g + i) + e]) =
+            make_float4(st.acc[e][i], st.acc[e + 1][i], st.acc[e + 2][i], st.acc[e + 3][i]);
+    if (g == 0) {
+      m[hd] = st.m;
+      l[hd] = st.l;
+    }
   }
 }
 
@@ -302,26 +339,68 @@ template <typename T, int D, int GP, bool kSplit>
 __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs a) {
   using Q = QuantBlock<D>;
   constexpr int NP = sizeof(T) == 2 ? 1 : 3;
-  const int bh = kSplit ? blockIdx.x / a.P : blockIdx.x, part = kSplit ? blockIdx.x % a.P : 0;
-  const int b = bh / a.Hkv, kvh = bh % a.Hkv;
+  constexpr bool kAhead = NP == 1 || D == 64;  // registers for a second unit
+  const int kvh = blockIdx.x, b = blockIdx.y, part = kSplit ? blockIdx.z : 0;
+  const int bh = b * gridDim.x + kvh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int hd = lane & 15, g = lane >> 4;
-  uint8_t* cache = a.cache + (size_t)bh * a.NB * Q::kBytes;
-  const float* logc = a.logc + (size_t)bh * a.Rcap;
 
-  __shared__ float s_acc[2][kWaves][GP][D];
+  __shared__ __align__(16) float s_acc[2][kWaves][GP][D];
   __shared__ float s_m[2][kWaves][GP];  // per kind (0 residual, 1 main), per wave
   __shared__ float s_l[2][kWaves][GP];
+  __shared__ float s_w[2][kWaves][GP];
   __shared__ __align__(16) uint16_t s_q[NP][GP][D];
   __shared__ double2 s_cs[64];
 
-  int r, n;
-  cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
-  const bool app = a.k_new != nullptr && r + n < a.C;
+  // The arguments that the first requests need, read together: left to where
+  // each is used, they came in a chain of six reads of up to 500 clocks.
+  const int32_t* positions = a.positions;
+  const int32_t* res_len = a.res_len;
+  const int32_t* main_len = a.main_len;
+  const T* qp = static_cast<const T*>(a.q);
+  const T* kp = static_cast<const T*>(a.k_new);
+  const T* vp = static_cast<const T*>(a.v_new);
+  uint8_t* cache = a.cache;
+  const float* logc = a.logc;
+  const double* freqs = a.rope.freq;
+  const int rot = a.rope.rot_dim, layout = a.rope.layout, G = a.G, NB = a.NB, Rcap = a.Rcap, C = a.C, W = a.W;
+  asm volatile("" ::"s"(positions), "s"(res_len), "s"(main_len), "s"(qp), "s"(kp), "s"(vp), "s"(cache), "s"(logc),
+               "s"(freqs), "s"(rot), "s"(layout), "s"(G), "s"(NB), "s"(Rcap), "s"(C), "s"(W));
+  cache += (size_t)bh * NB * Q::kBytes;
+  logc += (size_t)bh * Rcap;
+  const int begin = part * W;
+
+  // Requests that wait for nothing more, in the order of their use: the queries and
+  // this step's token with the partners of their elements, then the wave's first
+  // unit. (A wait for one load is a wait for all before it.)
+  constexpr int kQ = (GP * D + kThreads - 1) / kThreads;
+  const int pos = *(positions ? positions + b : res_len + bh);  // unused without a rotation
+  const int r_raw = res_len[bh], n_raw = main_len[bh];
+  const PairIndex at(positions ? rot : 0, layout);
+  double freq = 0.0;
+  if (at.rot) freq = freqs[min(lane, rot / 2 - 1)];
+  PairElem<T> qe[kQ], ne[2];
+  qp += (size_t)bh * G * D;
+#pragma unroll
+  for (int k = 0; k < kQ; ++k) {
+    const int i = tid + k * kThreads;
+    qe[k].load(qp + min(i / D, G - 1) * D, i % D, at);
+  }
+  const PairIndex at_new(wave ? 0 : at.rot, layout);
+  const int l_new = min(lane, D / 2 - 1);
+  const T* new_row = kp ? (wave ? vp : kp) + (size_t)bh * D : qp;  // wave 0 has the key, wave 1 the value
+  ne[0].load(new_row, 2 * l_new, at_new);
+  ne[1].load(new_row, 2 * l_new + 1, at_new);
+  Unit<D> u;
+  u.load(cache, min(begin + wave, NB - 1), logc, Rcap, lane);
+  __builtin_amdgcn_sched_barrier(0);  // no wait for any of them before the last is on its way
+  const int r = clampi(r_raw, 0, min(Rcap, C));  // as cache_lengths
+  int n = clampi(n_raw, 0, C - r);
+  const bool app = kp != nullptr && r + n < C;
   const int app_slot = r + n;
   if (app) n += 1;
   const int total = r + n;
-  const int begin = part * a.W, end = min(begin + a.W, (total + kUnit - 1) / kUnit);
+  const int end = min(begin + W, (total + kUnit - 1) / kUnit);
   if (kSplit && begin >= end) {  // no live slot here: records without weight
     for (int i = tid; i < 2 * GP; i += kThreads) {
       float* ml = a.rec_ml + (((size_t)bh * a.P + part) * 2 * GP + i) * 2;
@@ -330,24 +409,16 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
     }
     return;
   }
-  const int rot = a.positions ? a.rope.rot_dim : 0;
-  if (tid < rot / 2) s_cs[tid] = turn(a.rope.freq[tid], a.positions[b], a.rope.attn_scale);
-  __syncthreads();
-  // this step's token into the cache (wave 0 the key, wave 1 the value)
-  if (app && wave < 2 && app_slot / kUnit >= begin && app_slot / kUnit < end) {
-    const T* src = static_cast<const T*>(wave ? a.v_new : a.k_new) + (size_t)bh * D;
-    const int l = min(lane, D / 2 - 1), rk = wave ? 0 : rot;
-    store_row_quant<D>(cache + (size_t)(app_slot / kUnit) * Q::kBytes, app_slot % kUnit, wave == 1,
-                       rotated_elem(src, 2 * l, rk, a.rope.layout, s_cs),
-                       rotated_elem(src, 2 * l + 1, rk, a.rope.layout, s_cs), lane);
+  if (at.rot) {
+    if (tid < 64) s_cs[tid] = turn(freq, pos, a.rope.attn_scale);
+    __syncthreads();
   }
   // queries, rotated, as bf16 parts
-  for (int i = tid; i < GP * D; i += kThreads) {
-    const int h = i / D, e = i % D;
-    float x = 0.f;
-    if (h < a.G)
-      x = rotated_elem(static_cast<const T*>(a.q) + ((size_t)b * a.Hq + (size_t)kvh * a.G + h) * D, e, rot,
-                       a.rope.layout, s_cs);
+#pragma unroll
+  for (int k = 0; k < kQ; ++k) {
+    const int i = tid + k * kThreads, h = i / D, e = i % D;
+    if (h >= GP) continue;
+    float x = h < G ? qe[k].rotated(e, at, s_cs) : 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const uint16_t w = f32_to_bf16_rne(x);
@@ -355,43 +426,50 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
       x -= __uint_as_float((uint32_t)w << 16);
     }
   }
+  const int app_blk = app && app_slot / kUnit >= begin && app_slot / kUnit < end ? app_slot / kUnit : -1;
+  if (app_blk >= 0 && wave < 2)
+    store_row_quant<D>(cache + (size_t)app_blk * Q::kBytes, app_slot % kUnit, wave == 1,
+                       ne[0].rotated(2 * l_new, at_new, s_cs), ne[1].rotated(2 * l_new + 1, at_new, s_cs), lane);
   __syncthreads();
   Row<D> q[NP];
+  const int hq = kPaired<GP> ? hd & 7 : hd;  // query head of this lane's column
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
-      q[p].s[i] = hd < GP ? *reinterpret_cast<const uint4*>(&s_q[p][hd][g * (D / 4) + 8 * i]) : make_uint4(0, 0, 0, 0);
+      q[p].s[i] = hq < GP ? *reinterpret_cast<const uint4*>(&s_q[p][hq][g * (D / 4) + 8 * i]) : make_uint4(0, 0, 0, 0);
+  if (app_blk == begin + wave) u.load(cache, app_blk, logc, Rcap, lane);  // with the new token
 
-  // The waves take the cache blocks in turn; residual slots come first, and the
-  // block that holds slot r has a part of each kind.
+  // The waves take the cache blocks in turn, the next one requested before the
+  // present one is worked on; residual slots come first, and the block that holds
+  // slot r has a part of each kind.
   State<D> st;
   st.reset();
   bool in_res = true;
-  for (int blk = begin + wave; blk < end; blk += kWaves) {
-    Unit<D> u;
-    u.load(cache + (size_t)blk * Q::kBytes, hd, g);
+  auto work = [&](const Unit<D>& u, int blk) __attribute__((always_inline)) {
     const int s0 = blk * kUnit;
-    float lc[kTiles][4] = {};
-    if (s0 < r) {
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = s0 + 16 * t + 4 * g + i;
-          lc[t][i] = j < r ? logc[j] : 0.f;
-        }
-    }
     float s[kTiles][4];
-    unit_logits<D, NP>(u, q, a.qk_scale, s);
-    if (s0 < r) softmax_pv<D>(st, u, s, lc, 0, r - s0, true, a.beta_log2, g);
-    if (s0 + kUnit > r && s0 < total) {
-      if (in_res) {
+    unit_logits<D, NP>(u, q, s);
+    const int last = s0 + kUnit > r ? 1 : 0;
+    for (int kind = s0 < r ? 0 : 1; kind <= last; ++kind) {
+      if (kind == 1 && in_res) {
         store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
         st.reset();
         in_res = false;
       }
-      softmax_pv<D>(st, u, s, lc, r - s0, total - s0, false, 0.f, g);
+      softmax_pv<D, GP>(st, u, s, kind ? r - s0 : 0, (kind ? total : r) - s0, kind == 0, a.qk_scale, a.beta_log2, hd,
+                        g);
+    }
+  };
+  for (int blk = begin + wave; blk < end; blk += kWaves) {
+    if constexpr (kAhead) {
+      Unit<D> next;
+      next.load(cache, min(blk + kWaves, end - 1), logc, Rcap, lane);
+      work(u, blk);
+      u = next;
+    } else {
+      if (blk != begin + wave) u.load(cache, blk, logc, Rcap, lane);
+      work(u, blk);
     }
   }
   if (in_res) {
@@ -401,47 +479,69 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
   store_state<D, GP>(st, s_acc[1][wave], s_m[1][wave], s_l[1][wave], hd, g);
   __syncthreads();
 
-  // (head h, column d) of one kind over the waves
-  auto merge = [&](int kind, int h, int d, float& M, float& l, float& o) {
-    M = s_m[kind][0][h];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[kind][w][h]);
-    o = 0.f;
-    l = 0.f;
-    if (M != kNegInf) {
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2f(s_m[kind][w][h] - M);
-        o = fmaf(f, s_acc[kind][w][h][d], o);
-        l = fmaf(f, s_l[kind][w][h], l);
+  // Weights of the waves' states: 16 lanes a head, lane 8 kind + w of wave w's.
+  // Sums within 8 lanes by neighbours, pairs and the mirror of 8, which meets the
+  // four lanes that hold the other partial sum.
+  if (tid < 16 * GP) {
+    const int h = tid >> 4, kind = (tid >> 3) & 1, w = tid & 7;
+    const float m = s_m[kind][w][h], l = s_l[kind][w][h];
+    float M = m;
+    M = fmaxf(M, dpp_move<0xB1>(M));
+    M = fmaxf(M, dpp_move<0x4E>(M));
+    M = fmaxf(M, dpp_move<0x141>(M));
+    const float f = m != kNegInf ? exp2f(m - M) : 0.f;
+    float L = m != kNegInf ? f * l : 0.f;
+    L += dpp_move<0xB1>(L);
+    L += dpp_move<0x4E>(L);
+    L += dpp_move<0x141>(L);
+    if constexpr (kSplit) {
+      s_w[kind][w][h] = f;
+      if (w == 0) {
+        float* ml = a.rec_ml + (((size_t)bh * a.P + part) * 2 * GP + kind * GP + h) * 2;
+        ml[0] = M;
+        ml[1] = L;
+      }
+    } else {
+      const float Mo = dpp_move<0x128>(M), Lo = dpp_move<0x128>(L);  // the other kind's (row_ror:8)
+      const float mM = kind ? M : Mo, lM = kind ? L : Lo, mR = kind ? Mo : M, lR = kind ? Lo : L;
+      if (h < G) {
+        const int qh = bh * G + h;
+        const Joined j = join(a, qh, mM, lM, mR, lR);
+        s_w[kind][w][h] = f * (kind ? j.fM : j.fR) * j.inv;
+        if ((tid & 15) == 0) write_stats(a, qh, mM, lM, mR, lR, j.gate);
       }
     }
-  };
-  if constexpr (kSplit) {
-    for (int i = tid; i < 2 * GP * D; i += kThreads) {
-      const int kind = i / (GP * D), h = i / D % GP, d = i % D;
-      float M, l, o;
-      merge(kind, h, d, M, l, o);
-      const size_t row = ((size_t)bh * a.P + part) * 2 * GP + kind * GP + h;
-      if (M != kNegInf) a.rec_acc[row * D + d] = o;
-      if (d == 0) {
-        a.rec_ml[row * 2] = M;
-        a.rec_ml[row * 2 + 1] = l;
-      }
-    }
-  } else {
-    for (int i = tid; i < a.G * D; i += kThreads) {
-      const int h = i / D, d = i % D;
-      float mR, lR, oR, mM, lM, oM;
-      merge(0, h, d, mR, lR, oR);
-      merge(1, h, d, mM, lM, oM);
-      const int qh = b * a.Hq + kvh * a.G + h;
-      const Joined j = join(a, qh, mM, lM, mR, lR);
-      a.out[(size_t)qh * D + d] = (oM * j.fM + oR * j.fR) * j.inv;
-      if (d == 0) write_stats(a, qh, mM, lM, mR, lR, j.gate);
-    }
-    if (app && tid == 0) a.main_len[bh] = n;
   }
+  __syncthreads();
+  // the outputs, four columns a thread
+  const bool has_res = begin * kUnit < r, has_main = end * kUnit > r && total > r;
+  auto weighed = [&](int kind, int h, int d) {
+    f32x4_t o = zero4();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = s_w[kind][w][h];
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&s_acc[kind][w][h][d]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = fmaf(f, v[i], o[i]);
+    }
+    return o;
+  };
+  for (int i = tid; i < G * (D / 4); i += kThreads) {
+    const int h = i / (D / 4), d = i % (D / 4) * 4;
+    if constexpr (kSplit) {
+      float* rec = a.rec_acc + (((size_t)bh * a.P + part) * 2 * GP + h) * D + d;
+      if (has_res) *reinterpret_cast<f32x4_t*>(rec) = weighed(0, h, d);
+      if (has_main) *reinterpret_cast<f32x4_t*>(rec + GP * D) = weighed(1, h, d);
+    } else {
+      f32x4_t o = zero4();
+      if (has_main) o = weighed(1, h, d);
+      if (has_res) o += weighed(0, h, d);
+      float* out = a.out + ((size_t)bh * G + h) * D + d;  // 4-byte aligned
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = o[k];
+    }
+  }
+  if (!kSplit && app && tid == 0) a.main_len[bh] = n;
 }
 
 // Join the records of one query head: one block of D threads, thread d a column.
@@ -450,7 +550,7 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
 // group's first head, which alone reads it.
 template <int D, int GP>
 __global__ __launch_bounds__(D) void decode_quant_combine(QuantDecodeArgs a) {
-  const int bh = blockIdx.x / a.G, h = blockIdx.x % a.G, b = bh / a.Hkv, kvh = bh % a.Hkv;
+  const int h = blockIdx.x, bh = blockIdx.z * gridDim.y + blockIdx.y;
   const int d = threadIdx.x, lane = d & 63;
   __shared__ float s_w[2 * kMaxParts];
   const size_t row0 = (size_t)bh * a.P * 2 * GP + h;  // record i = 2 p + kind is row i GP further
@@ -474,7 +574,7 @@ __global__ __launch_bounds__(D) void decode_quant_combine(QuantDecodeArgs a) {
 #pragma unroll
   for (int x = 2; x < 64; x <<= 1) sum = wave_xor_add(sum, x);
   const float mR = __shfl(own, 0, 64), mM = __shfl(own, 1, 64), lR = __shfl(sum, 0, 64), lM = __shfl(sum, 1, 64);
-  const int qh = b * a.Hq + kvh * a.G + h;
+  const int qh = bh * a.G + h;
   const Joined j = join(a, qh, mM, lM, mR, lR);
   if (d < 64) {
 #pragma unroll
@@ -507,11 +607,11 @@ __global__ __launch_bounds__(D) void decode_quant_combine(QuantDecodeArgs a) {
 template <typename T, int D, int GP>
 void launch_kernels(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStream_t stream) {
   if (pl.P == 1) {
-    hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, false>), dim3(pl.BH), dim3(kThreads), 0, stream, da);
+    hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, false>), dim3(pl.Hkv, pl.B), dim3(kThreads), 0, stream, da);
     return;
   }
-  hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.BH * pl.P), dim3(kThreads), 0, stream, da);
-  hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(pl.BH * da.G), dim3(D), 0, stream, da);
+  hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.Hkv, pl.B, pl.P), dim3(kThreads), 0, stream, da);
+  hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(da.G, pl.Hkv, pl.B), dim3(D), 0, stream, da);
 }
 
 template <typename T, int D>
@@ -530,19 +630,21 @@ hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipSt
 
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   QuantDecodePlan p{};
-  p.BH = s.batch * s.num_kv_heads;
+  p.B = s.batch;
+  p.Hkv = s.num_kv_heads;
+  const long long BH = (long long)p.B * p.Hkv;
   const int G = s.num_q_heads / s.num_kv_heads;
   p.GP = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : G <= 8 ? 8 : 16;
   const int NB = (s.slot_cap + kUnit - 1) / kUnit;
   p.P = 1;
   p.W = NB;
-  if (p.BH < 256 && NB > 2 * kWaves) {
-    const int want = 256 / p.BH < kMaxParts ? 256 / p.BH : kMaxParts;
+  if (BH < 256 && NB > 2 * kWaves) {
+    const int want = 256 / (int)BH < kMaxParts ? 256 / (int)BH : kMaxParts;
     p.W = (NB + want - 1) / want;
     p.W = (p.W + kWaves - 1) / kWaves * kWaves;
     p.P = (NB + p.W - 1) / p.W;
   }
-  const size_t rows = p.P > 1 ? (size_t)p.BH * p.P * 2 * p.GP : 0;
+  const size_t rows = p.P > 1 ? (size_t)BH * p.P * 2 * p.GP : 0;
   p.acc_off = align_up(rows * 2 * sizeof(float), 256);
   p.bytes = align_up(p.acc_off + rows * s.head_dim * sizeof(float), 256) + 256;  // never 0
   return p;
@@ -563,7 +665,7 @@ hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, co
   da.rec_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.acc_off);
   da.P = pl.P; da.W = pl.W;
   da.dbg_lse_main = dbg_lse_main; da.dbg_lse_res = dbg_lse_res; da.dbg_gate = dbg_gate;
-  da.Hq = s.num_q_heads; da.Hkv = s.num_kv_heads; da.G = s.num_q_heads / s.num_kv_heads;
+  da.G = s.num_q_heads / s.num_kv_heads;
   da.C = s.slot_cap; da.Rcap = s.res_cap; da.NB = (s.slot_cap + kUnit - 1) / kUnit;
   da.qk_scale = kLog2e / sqrtf((float)s.head_dim);
   da.beta_log2 = g.beta * kLog2e;

@@ -66,7 +66,7 @@ hipError_t launch_append(const reskv_shape_t& s, const void* k_new, const void* 
                          void* vc, const int32_t* res_len, int32_t* main_len, hipStream_t stream);
 
 // Rotary positions.
-void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope);
+void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope, double* freq);
 hipError_t launch_rope(const reskv_shape_t& s, const reskv_rope_t& rope, int n_rows, const int32_t* positions,
                        const int32_t* n_tok, const void* q, const reskv_rows_t* q_at, void* q_out,
                        const reskv_rows_t* q_out_at, const void* k, const reskv_rows_t* k_at, void* k_out,
@@ -84,7 +84,7 @@ hipError_t launch_append_quant(const reskv_shape_t& s, const reskv_rope_t* rope,
                                const int32_t* res_len, int32_t* main_len, hipStream_t stream);
 
 struct QuantDecodePlan {
-  int BH, GP;
+  int B, Hkv, GP;
   int P, W;  // blocks a (b, kv head) is split over, 64-slot cache blocks of each
   size_t acc_off, bytes;
 };

@@ -138,18 +138,20 @@ __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
     const int t = row >> 1;
     const bool value = row & 1;
     const T* src = static_cast<const T*>(value ? a.v_new : a.k_new) + ((size_t)bh * a.n_new + t) * D;
-    float x = elem(src, 2 * l), y = elem(src, 2 * l + 1);
-    if (!value && a.positions) {
+    const PairIndex at(!value && a.positions ? a.rope.rot_dim : 0, a.rope.layout);
+    PairElem<T> x, y;
+    x.load(src, 2 * l, at);
+    y.load(src, 2 * l + 1, at);
+    if (at.rot) {
       if (lane < a.rope.rot_dim / 2)
         s_cs[wave][lane] = turn(a.rope.freq[lane], a.positions[(size_t)b * a.n_new + t], a.rope.attn_scale);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      x = rotated_elem(src, 2 * l, a.rope.rot_dim, a.rope.layout, s_cs[wave]);
-      y = rotated_elem(src, 2 * l + 1, a.rope.rot_dim, a.rope.layout, s_cs[wave]);
-      __builtin_amdgcn_wave_barrier();
     }
     const int slot = r + n + t;
-    store_row_quant<D>(head + (size_t)(slot / 64) * Q::kBytes, slot % 64, value, x, y, lane);
+    store_row_quant<D>(head + (size_t)(slot / 64) * Q::kBytes, slot % 64, value,
+                       x.rotated(2 * l, at, s_cs[wave]), y.rotated(2 * l + 1, at, s_cs[wave]), lane);
+    __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();  // every wave has read the lengths
   if (tid == 0 && take > 0) a.main_len[bh] = n + take;

@@ -96,11 +96,12 @@ void launch(const RopeArgs& ra, hipStream_t stream) {
 
 }  // namespace
 
-void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope) {
+void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope, double* freq) {
   const double kTwoPi = 6.283185307179586;
   const int rot = p.rot_dim;
   rope->rot_dim = rot;
   rope->layout = p.layout;
+  rope->freq = nullptr;
   rope->attn_scale = p.attn_scale;
   if (p.attn_scale == 0.0) rope->attn_scale = p.scaling == RESKV_ROPE_YARN ? 0.1 * log(p.factor) + 1.0 : 1.0;
   const double base = p.scaling == RESKV_ROPE_NTK ? p.theta * pow(p.factor, rot / (rot - 2.0)) : p.theta;
@@ -110,11 +111,7 @@ void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope) {
     lo = fmax(floor(dim(p.beta_fast)), 0.0);
     hi = fmin(ceil(dim(p.beta_slow)), rot - 1.0);
   }
-  for (int i = 0; i < 64; ++i) {
-    if (i >= rot / 2) {
-      rope->freq[i] = 0.0;
-      continue;
-    }
+  for (int i = 0; i < rot / 2; ++i) {
     double f = pow(base, -2.0 * i / rot);
     if (p.scaling == RESKV_ROPE_LINEAR) f /= p.factor;
     if (p.scaling == RESKV_ROPE_LLAMA3) {
@@ -127,7 +124,7 @@ void make_rope(const reskv_rope_params_t& p, reskv_rope_t* rope) {
       const double t = fmin(fmax((i - lo) / fmax(hi - lo, 0.001), 0.0), 1.0);
       f = f / p.factor * t + f * (1.0 - t);
     }
-    rope->freq[i] = f;
+    freq[i] = f;
   }
 }
 

@@ -43,19 +43,40 @@ __device__ __forceinline__ float round_to(double v, const uint16_t*) {
 __device__ __forceinline__ float elem(const uint16_t* row, int i) { return __uint_as_float((uint32_t)row[i] << 16); }
 __device__ __forceinline__ float elem(const float* row, int i) { return row[i]; }
 
-// Element i of a row, rotated with the turns cs[pair] of its position.
-template <typename T>
-__device__ __forceinline__ float rotated_elem(const T* row, int i, int rot, int layout, const double2* cs) {
-  if (i >= rot) return elem(row, i);
-  double xr, yr;
-  if (layout == RESKV_ROPE_HALF) {
-    const int p = i < rot / 2 ? i : i - rot / 2;
-    rotate_pair(elem(row, p), elem(row, p + rot / 2), cs[p], xr, yr);
-    return round_to(i < rot / 2 ? xr : yr, row);
+// Where element i of a row has the other one of its pair: index arithmetic that
+// holds for both layouts, without branches.
+struct PairIndex {
+  int rot, half, odd, lim;  // half: rot / 2 in the half layout, else 0; odd: 1 in the interleaved one
+  __device__ __forceinline__ PairIndex(int rot_dim, int layout) {
+    const bool h = layout == RESKV_ROPE_HALF;
+    rot = rot_dim;
+    half = h ? rot_dim / 2 : 0;
+    odd = h ? 0 : 1;
+    lim = h ? rot_dim / 2 : rot_dim;
   }
-  const int p = i >> 1;
-  rotate_pair(elem(row, 2 * p), elem(row, 2 * p + 1), cs[p], xr, yr);
-  return round_to(i & 1 ? yr : xr, row);
-}
+  __device__ __forceinline__ bool turned(int i) const { return i < rot; }
+  __device__ __forceinline__ bool first(int i) const { return !(i & odd) && i < lim; }  // the pair's x
+  __device__ __forceinline__ int pair(int i) const { return (i >> odd) - (i < lim ? 0 : half); }
+  // (some element of the row for i >= rot)
+  __device__ __forceinline__ int other(int i) const { return (i ^ odd) + (i < lim ? half : -half); }
+};
+// Element i of a row as stored, with its pair's other element; rotated once the
+// turns cs[pair] of the row's position are known, and rounded to T.
+template <typename T>
+struct PairElem {
+  T own, other;
+  __device__ __forceinline__ void load(const T* row, int i, const PairIndex& at) {
+    own = row[i];
+    other = row[at.other(i)];
+  }
+  __device__ __forceinline__ float rotated(int i, const PairIndex& at, const double2* cs) const {
+    const float x = elem(&own, 0), y = elem(&other, 0);
+    if (!at.turned(i)) return x;
+    const bool first = at.first(i);
+    double xr, yr;
+    rotate_pair(first ? x : y, first ? y : x, cs[at.pair(i)], xr, yr);
+    return round_to(first ? xr : yr, &own);
+  }
+};
 
 }  // namespace reskv

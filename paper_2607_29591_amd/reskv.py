@@ -54,7 +54,7 @@ class RopeParams(ctypes.Structure):
 
 class Rope(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("attn_scale", ctypes.c_double),
-                ("freq", ctypes.c_double * 64)]
+                ("freq", ctypes.c_void_p)]
 
 
 class Rows(ctypes.Structure):
@@ -96,7 +96,7 @@ _SIG = {
                                              _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "reskv_merge_branches": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P]),
     "reskv_append_kv": (ctypes.c_int, [ctypes.POINTER(Shape), _P, _P, _P, _P, _P, _P, _P]),
-    "reskv_rope_init": (ctypes.c_int, [ctypes.POINTER(RopeParams), ctypes.POINTER(Rope)]),
+    "reskv_rope_init": (ctypes.c_int, [ctypes.POINTER(RopeParams), ctypes.POINTER(Rope), _P]),
     "reskv_rope": (ctypes.c_int, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.c_int32, _P, _P, _P,
                                   ctypes.POINTER(Rows), _P, ctypes.POINTER(Rows), _P, ctypes.POINTER(Rows), _P,
                                   ctypes.POINTER(Rows), _P]),
@@ -352,12 +352,28 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "llama3": 3, "yarn": 4}
 
 def make_rope(rot_dim, layout="half", theta=10000.0, scaling="none", factor=1.0, original_len=0.0,
               low_freq_factor=1.0, high_freq_factor=4.0, beta_fast=32.0, beta_slow=1.0, attn_scale=0.0):
-    """Rotation plan (reskv_rope_init); attn_scale 0 takes the scaling's own factor."""
+    """Rotation plan (reskv_rope_init); attn_scale 0 takes the scaling's own factor. The frequencies are on the plan
+    as the array freq_host and, where there is a GPU, in a tensor of the current one: make a plan outside of captures."""
+    import torch
     p = RopeParams(rot_dim, ROPE_LAYOUTS.get(layout, layout), ROPE_SCALINGS.get(scaling, scaling), theta, factor,
                    original_len, low_freq_factor, high_freq_factor, beta_fast, beta_slow, attn_scale)
-    rope = Rope()
-    _check(lib().reskv_rope_init(ctypes.byref(p), ctypes.byref(rope)))
+    rope, freq = Rope(), np.zeros(64)
+    _check(lib().reskv_rope_init(ctypes.byref(p), ctypes.byref(rope), freq.ctypes.data))
+    rope.freq_host = freq[:rot_dim // 2].copy()
+    if torch.cuda.is_available():
+        rope.table = torch.from_numpy(rope.freq_host).to("cuda")
+        rope.freq = rope.table.data_ptr()
     return rope
+
+
+def _rope(rope):
+    """Reference to a plan whose frequencies are on the current GPU (None -> NULL)."""
+    if rope is None:
+        return None
+    table = getattr(rope, "table", None)
+    if table is not None:
+        _tensor("the plan's frequencies", table, table.dtype, rope.rot_dim // 2)
+    return ctypes.byref(rope)
 
 
 def _tensor(name, t, dtype, count, contiguous=True):
@@ -407,7 +423,7 @@ def prepare_rope(shape, rope, positions, q=None, q_out=None, k=None, k_out=None,
             raise ValueError(f"{name} must be [{B}, {heads}, {n}, {d}] with adjoining elements, got {tuple(x.shape)} "
                              f"by {x.stride()}")
         at += [_tensor(name, x, _dtype(shape), x.numel(), False), ctypes.byref(Rows(*x.stride()[:3]))]
-    args = (ctypes.byref(shape), ctypes.byref(rope), n, _tensor("positions", positions, torch.int32, B * n),
+    args = (ctypes.byref(shape), _rope(rope), n, _tensor("positions", positions, torch.int32, B * n),
             _tensor("n_tok", n_tok, torch.int32, B), *at, _stream(stream))
     return _prepared(lib().reskv_rope, args, (shape, rope))
 
@@ -462,7 +478,7 @@ def reskv_unpack_quant(shape, cache, res_len, main_len, kc, vc, first_slot=None,
 
 def _turn(shape, rope, positions, n):
     import torch
-    return (None if rope is None else ctypes.byref(rope),
+    return (_rope(rope),
             _tensor("positions", positions, torch.int32, shape.batch * n))
 
 
