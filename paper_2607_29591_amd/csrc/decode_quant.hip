@@ -222,8 +222,9 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
 // say does not enter. A unit full of main slots needs none of that.
 template <int D, int GP>
 __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const float (&s)[kTiles][4],
-                                           int lo, int hi, bool is_res, float qk_scale, float beta_log2, int hd,
-                                           int g) {
+                                           int lo, int hi, bool is_res, float qk_scale, float beta_log2, float* s_bias,
+                                           int lane) {
+  const int hd = lane & 15, g = lane >> 4;
   float p[kTiles][4], vs[kTiles][4];
   float top = kNegInf, m_new, mu;
 #pragma unroll
@@ -245,16 +246,19 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(fmaf(s[t][i], qk_scale, -mu));
   } else {
-    const float from = is_res ? u.lc : 0.f;
+    // what a slot's logits are moved by (-inf: no weight), from the lane of the
+    // slot to the lanes of its logits
+    const bool weighs = lane >= lo && lane < hi && !(is_res && u.lc == kNegInf);
+    s_bias[lane] = !weighs ? kNegInf : is_res ? beta_log2 * u.lc : 0.f;
+    f32x4_t bias[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) bias[t] = *reinterpret_cast<const f32x4_t*>(&s_bias[16 * t + 4 * g]);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int j = 16 * t + 4 * g + i;
-        const float lc = __shfl(from, j, 64);
-        const bool live = j >= lo && j < hi && lc != kNegInf;
-        const float v = s[t][i] * qk_scale + beta_log2 * lc;
-        p[t][i] = live ? v : kNegInf;
+        const bool live = bias[t][i] != kNegInf;
+        p[t][i] = live ? fmaf(s[t][i], qk_scale, bias[t][i]) : kNegInf;
         vs[t][i] = live ? vs[t][i] : 0.f;
         top = fmaxf(top, p[t][i]);
       }
@@ -349,6 +353,7 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
   __shared__ float s_m[2][kWaves][GP];  // per kind (0 residual, 1 main), per wave
   __shared__ float s_l[2][kWaves][GP];
   __shared__ float s_w[2][kWaves][GP];
+  __shared__ __align__(16) float s_bias[kWaves][kUnit];
   __shared__ __align__(16) uint16_t s_q[NP][GP][D];
   __shared__ double2 s_cs[64];
 
@@ -457,21 +462,23 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
         st.reset();
         in_res = false;
       }
-      softmax_pv<D, GP>(st, u, s, kind ? r - s0 : 0, (kind ? total : r) - s0, kind == 0, a.qk_scale, a.beta_log2, hd,
-                        g);
+      softmax_pv<D, GP>(st, u, s, kind ? r - s0 : 0, (kind ? total : r) - s0, kind == 0, a.qk_scale, a.beta_log2,
+                        s_bias[wave], lane);
     }
   };
-  for (int blk = begin + wave; blk < end; blk += kWaves) {
+  int blk = begin + wave;
+  for (; blk + kWaves < end; blk += kWaves) {
     if constexpr (kAhead) {
       Unit<D> next;
-      next.load(cache, min(blk + kWaves, end - 1), logc, Rcap, lane);
+      next.load(cache, blk + kWaves, logc, Rcap, lane);
       work(u, blk);
       u = next;
     } else {
-      if (blk != begin + wave) u.load(cache, blk, logc, Rcap, lane);
       work(u, blk);
+      u.load(cache, blk + kWaves, logc, Rcap, lane);
     }
   }
+  if (blk < end) work(u, blk);  // on its own: nothing more to request or to wait for
   if (in_res) {
     store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
     st.reset();
