@@ -338,6 +338,8 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
   if (st != RESKV_OK) return st;
   if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
   if (n_rows == 0) return ok();  // tensors without elements may have no address
+  if ((int64_t)shape->batch * n_rows > INT32_MAX)
+    return fail(RESKV_ERR_UNSUPPORTED, "%d sequences of %d rows are more than 2^31 - 1", shape->batch, n_rows);
   if (!rope || !positions) return fail(RESKV_ERR_INVALID_ARG, "rope or positions is NULL");
   if ((st = check_rope(shape, rope)) != RESKV_OK) return st;
   if (!q && !q_out && !k && !k_out) return fail(RESKV_ERR_INVALID_ARG, "neither queries nor keys are given");
@@ -349,13 +351,22 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
   return ok();
 }
 
+// Shapes of the 4-bit caches: sequences and heads are dimensions of the grids.
+static reskv_status_t check_quant_shape(const reskv_shape_t* s) {
+  reskv_status_t st = check_shape(s);
+  if (st != RESKV_OK) return st;
+  if (s->batch > 65535 || s->num_kv_heads > 32767)
+    return fail(RESKV_ERR_UNSUPPORTED, "batch %d above 65535 or %d KV heads above 32767", s->batch, s->num_kv_heads);
+  return RESKV_OK;
+}
+
 size_t reskv_quant_cache_size(const reskv_shape_t* shape) {
-  return check_shape(shape) == RESKV_OK ? quant_cache_bytes(*shape) : 0;
+  return check_quant_shape(shape) == RESKV_OK ? quant_cache_bytes(*shape) : 0;
 }
 
 reskv_status_t reskv_pack_quant(const reskv_shape_t* shape, const void* kc, const void* vc, const int32_t* res_len,
                                 const int32_t* main_len, void* cache, void* stream) {
-  reskv_status_t st = check_shape(shape);
+  reskv_status_t st = check_quant_shape(shape);
   if (st != RESKV_OK) return st;
   if (!kc || !vc || !res_len || !main_len || !cache) return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
   if (!aligned(kc) || !aligned(vc) || !aligned(cache))
@@ -368,7 +379,7 @@ reskv_status_t reskv_pack_quant(const reskv_shape_t* shape, const void* kc, cons
 reskv_status_t reskv_unpack_quant(const reskv_shape_t* shape, const void* cache, const int32_t* res_len,
                                   const int32_t* main_len, const int32_t* first_slot, int32_t n_rows, void* kc,
                                   void* vc, void* stream) {
-  reskv_status_t st = check_shape(shape);
+  reskv_status_t st = check_quant_shape(shape);
   if (st != RESKV_OK) return st;
   if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
   if (n_rows == 0) return ok();
@@ -391,7 +402,7 @@ static reskv_status_t check_turn(const reskv_shape_t* shape, const reskv_rope_t*
 reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rope_t* rope, const int32_t* positions,
                                      int32_t n_new, const int32_t* n_tok, const void* k_new, const void* v_new,
                                      void* cache, const int32_t* res_len, int32_t* main_len, void* stream) {
-  reskv_status_t st = check_shape(shape);
+  reskv_status_t st = check_quant_shape(shape);
   if (st != RESKV_OK) return st;
   if (n_new < 0) return fail(RESKV_ERR_INVALID_ARG, "n_new %d must be >= 0", n_new);
   if (n_new == 0) return ok();
@@ -407,7 +418,7 @@ reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rop
 }
 
 size_t reskv_decode_quant_workspace_size(const reskv_shape_t* shape) {
-  return check_shape(shape) == RESKV_OK ? make_quant_decode_plan(*shape).bytes : 0;
+  return check_quant_shape(shape) == RESKV_OK ? make_quant_decode_plan(*shape).bytes : 0;
 }
 
 reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_gate_t* gate, const reskv_rope_t* rope,
@@ -415,7 +426,7 @@ reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_g
                                        const int32_t* res_len, int32_t* main_len, const void* k_new,
                                        const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
                                        float* dbg_gate, void* workspace, size_t workspace_bytes, void* stream) {
-  reskv_status_t st = check_shape(shape);
+  reskv_status_t st = check_quant_shape(shape);
   if (st != RESKV_OK) return st;
   if ((st = check_gate(gate)) != RESKV_OK) return st;
   if (!q || !cache || !logc || !res_len || !main_len || !out)
@@ -425,7 +436,6 @@ reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_g
     return fail(RESKV_ERR_INVALID_ARG, "k_new and v_new must both be given or both be NULL");
   if (!aligned(q) || !aligned(cache) || !aligned(k_new) || !aligned(v_new))
     return fail(RESKV_ERR_INVALID_ARG, "q, k_new, v_new and cache must be aligned to 16 bytes");
-  if (shape->batch > 65535) return fail(RESKV_ERR_UNSUPPORTED, "batch %d above 65535", shape->batch);
   const QuantDecodePlan plan = make_quant_decode_plan(*shape);
   if (!workspace || workspace_bytes < plan.bytes)
     return fail(RESKV_ERR_WORKSPACE, "decode needs %zu workspace bytes, got %zu", plan.bytes,

@@ -48,6 +48,14 @@ __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 w) {
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
+// 16-byte store; kStream: past the caches, for results that are larger than them.
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+template <bool kStream>
+__device__ __forceinline__ void store16(void* p, u32x4_t v) {
+  if constexpr (kStream) __builtin_nontemporal_store(v, static_cast<u32x4_t*>(p));
+  else *static_cast<u32x4_t*>(p) = v;
+}
+
 // wave64 butterflies over the lanes selected by the xor masks
 __device__ __forceinline__ float wave_xor_max(float v, int mask) {
   return fmaxf(v, __shfl_xor(v, mask, 64));

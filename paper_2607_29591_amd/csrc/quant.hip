@@ -10,103 +10,105 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ void load32_f32(const uint16_t* p, float (&x)[32]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) load8_f32(p + 8 * j, reinterpret_cast<float(&)[8]>(x[8 * j]));
-}
-__device__ __forceinline__ void load32_f32(const float* p, float (&x)[32]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) load8_f32(p + 8 * j, reinterpret_cast<float(&)[8]>(x[8 * j]));
-}
+// Both kernels: thread = 8 elements of a row, 4 lanes a group of 32, the lanes of
+// a wave along the rows; blockIdx.y = 2 (kv head) + (0 keys, 1 values), z = sequence.
+// The 4 bytes of codes of 8 elements adjoin in the key rows and, at d = 128, in the
+// value rows, where four neighbouring slots fill 256 bytes. Memory-bound; a thread
+// packs kUnroll units of its block's run so that as many reads are in flight (256 x
+// 2048 slots of 128, 340 MB: 69, 68, 64 us at 1, 2, 4; 8 x 512: 2.4, 2.6, 2.9).
+constexpr int kUnroll = 4;
 
-// Thread = one group of 32 elements of one row (index: pair, keys or values,
-// slot, group).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const T* kc, const T* vc, const int32_t* res_len,
-                                                        const int32_t* main_len, uint8_t* cache, int BH, int C,
+                                                        const int32_t* main_len, uint8_t* cache, int Hkv, int C,
                                                         int Rcap) {
   using Q = QuantBlock<D>;
-  const long long i = blockIdx.x * (long long)kThreads + threadIdx.x;
-  const int c = (int)(i % Q::kGroups);
-  long long rest = i / Q::kGroups;
-  const int slot = (int)(rest % C);
-  rest /= C;
-  const bool value = rest & 1;
-  const long long bh = rest >> 1;
-  if (bh >= BH) return;
+  const bool value = blockIdx.y & 1;
+  const int bh = blockIdx.z * Hkv + (blockIdx.y >> 1), e = (int)(threadIdx.x % (D / 8)) * 8;
+  constexpr int kSlots = kThreads / (D / 8);  // slots of a block's unit
+  const long long first = (long long)blockIdx.x * (kSlots * kUnroll) + threadIdx.x / (D / 8);
   int r, n;
-  cache_lengths(res_len, main_len, (int)bh, C, Rcap, r, n);
-  if (slot >= r + n) return;
-  float x[32];
-  load32_f32((value ? vc : kc) + ((size_t)bh * C + slot) * D + 32 * c, x);
-  uint32_t top = 0;
+  cache_lengths(res_len, main_len, bh, C, Rcap, r, n);
+  if (first >= r + n) return;  // the four lanes of a group alike
+  const T* src = (value ? vc : kc) + (size_t)bh * C * D + e;
+  uint8_t* head = cache + (size_t)bh * ((C + 63) / 64) * Q::kBytes;
+  float x[kUnroll][8];
 #pragma unroll
-  for (int k = 0; k < 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-  const uint32_t byte = scale_byte(top);
-  uint32_t w[4] = {0, 0, 0, 0};
+  for (int u = 0; u < kUnroll; ++u) load8_f32(src + min(first + u * kSlots, (long long)(r + n - 1)) * D, x[u]);
 #pragma unroll
-  for (int k = 0; k < 16; ++k) w[k / 4] |= code_pair(x[2 * k], x[2 * k + 1], scale_of(byte)) << (8 * (k % 4));
-  uint8_t* block = cache + ((size_t)bh * ((C + 63) / 64) + slot / 64) * Q::kBytes;
-  const int s = slot % 64;
-  if (value) {
-    constexpr int kW = Q::kPiece / 2;  // bytes of a piece: 4 or 2
+  for (int u = 0; u < kUnroll; ++u) {
+    const long long slot = first + u * kSlots;
+    uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < 16 / kW; ++k) {
-      uint8_t* at = block + Q::v_code(s, 32 * c / Q::kPiece + k);
-      if (kW == 4) *reinterpret_cast<uint32_t*>(at) = w[k % 4];
-      else *reinterpret_cast<uint16_t*>(at) = (uint16_t)(w[k / 2] >> (16 * (k % 2)));
+    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[u][k]) & 0x7fffffffu);
+    top = dpp_umax<0xB1>(top);
+    top = dpp_umax<0x4E>(top);
+    const uint32_t byte = scale_byte(top);
+    const float scale = scale_of(byte);
+    const uint32_t w = code_pair(x[u][0], x[u][1], scale) | code_pair(x[u][2], x[u][3], scale) << 8 |
+                       code_pair(x[u][4], x[u][5], scale) << 16 | code_pair(x[u][6], x[u][7], scale) << 24;
+    if (slot >= r + n) break;
+    uint8_t* block = head + (size_t)(slot / 64) * Q::kBytes;
+    const int s = (int)(slot % 64);
+    if (!value) {
+      *reinterpret_cast<uint32_t*>(block + Q::k_code(s) + e / 2) = w;
+    } else if (Q::kPiece == 8) {
+      *reinterpret_cast<uint32_t*>(block + Q::v_code(s, e / 8)) = w;
+    } else {
+      *reinterpret_cast<uint16_t*>(block + Q::v_code(s, e / 4)) = (uint16_t)w;
+      *reinterpret_cast<uint16_t*>(block + Q::v_code(s, e / 4 + 1)) = (uint16_t)(w >> 16);
     }
-  } else {
-    *reinterpret_cast<uint4*>(block + Q::k_code(s) + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (e % 32 == 0) block[value ? Q::v_scale(s, e / 32) : Q::k_scale(s, e / 32)] = (uint8_t)byte;
   }
-  block[value ? Q::v_scale(s, c) : Q::k_scale(s, c)] = (uint8_t)byte;
 }
 
+// Values of more bytes than the last-level cache holds (256 MB) are stored past the
+// caches: they would have left them before they are read again, and are written
+// faster so (256 x 2304 slots of 128 into 268 MB: 76 us through the caches, 49 past
+// them). Fewer stay where the next call finds them.
+constexpr double kStreamBytes = 256.0 * 1024 * 1024;
+
+template <bool kStream>
 __device__ __forceinline__ void store8_pairs(uint16_t* p, const uint32_t (&v)[4]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]);
+  store16<kStream>(p, u32x4_t{v[0], v[1], v[2], v[3]});
 }
+template <bool kStream>
 __device__ __forceinline__ void store8_pairs(float* p, const uint32_t (&v)[4]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1]));
-  reinterpret_cast<float4*>(p)[1] = make_float4(bf16_lo(v[2]), bf16_hi(v[2]), bf16_lo(v[3]), bf16_hi(v[3]));
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    store16<kStream>(p + 4 * k, u32x4_t{v[2 * k] << 16, v[2 * k] & 0xffff0000u, v[2 * k + 1] << 16,
+                                        v[2 * k + 1] & 0xffff0000u});
 }
 
-// Thread = one group of 32 elements of one output row.
-template <typename T, int D>
+template <typename T, int D, bool kStream>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t* cache, const int32_t* res_len,
                                                           const int32_t* main_len, const int32_t* first, int n_rows,
-                                                          T* kc, T* vc, int BH, int C, int Rcap) {
+                                                          T* kc, T* vc, int Hkv, int C, int Rcap) {
   using Q = QuantBlock<D>;
   const long long i = blockIdx.x * (long long)kThreads + threadIdx.x;
-  const int c = (int)(i % Q::kGroups);
-  long long rest = i / Q::kGroups;
-  const int row = (int)(rest % n_rows);
-  rest /= n_rows;
-  const bool value = rest & 1;
-  const long long bh = rest >> 1;
-  if (bh >= BH) return;
+  const long long row = i / (D / 8);
+  const int e = (int)(i % (D / 8)) * 8;
+  const bool value = blockIdx.y & 1;
+  const int bh = blockIdx.z * Hkv + (blockIdx.y >> 1);
   int r, n;
-  cache_lengths(res_len, main_len, (int)bh, C, Rcap, r, n);
-  const long long slot = (first ? first[bh] : 0) + (long long)row;
-  if (slot < 0 || slot >= r + n) return;
+  cache_lengths(res_len, main_len, bh, C, Rcap, r, n);
+  const long long slot = (first ? first[bh] : 0) + row;
+  if (row >= n_rows || slot < 0 || slot >= r + n) return;
   const uint8_t* block = cache + ((size_t)bh * ((C + 63) / 64) + slot / 64) * Q::kBytes;
   const int s = (int)(slot % 64);
-  const float scale = scale_of(block[value ? Q::v_scale(s, c) : Q::k_scale(s, c)]);
-  T* out = (value ? vc : kc) + ((size_t)bh * n_rows + row) * D + 32 * c;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {  // 8 elements: 4 bytes of codes
-    uint32_t w;
-    if (!value) {
-      w = *reinterpret_cast<const uint32_t*>(block + Q::k_code(s) + 16 * c + 4 * k);
-    } else if (Q::kPiece == 8) {
-      w = *reinterpret_cast<const uint32_t*>(block + Q::v_code(s, 4 * c + k));
-    } else {
-      w = *reinterpret_cast<const uint16_t*>(block + Q::v_code(s, 8 * c + 2 * k)) |
-          (uint32_t)*reinterpret_cast<const uint16_t*>(block + Q::v_code(s, 8 * c + 2 * k + 1)) << 16;
-    }
-    const uint32_t v[4] = {value_pair<0>(w, scale), value_pair<1>(w, scale), value_pair<2>(w, scale),
-                           value_pair<3>(w, scale)};
-    store8_pairs(out + 8 * k, v);
+  const float scale = scale_of(block[value ? Q::v_scale(s, e / 32) : Q::k_scale(s, e / 32)]);
+  uint32_t w;
+  if (!value) {
+    w = *reinterpret_cast<const uint32_t*>(block + Q::k_code(s) + e / 2);
+  } else if (Q::kPiece == 8) {
+    w = *reinterpret_cast<const uint32_t*>(block + Q::v_code(s, e / 8));
+  } else {
+    w = *reinterpret_cast<const uint16_t*>(block + Q::v_code(s, e / 4)) |
+        (uint32_t)*reinterpret_cast<const uint16_t*>(block + Q::v_code(s, e / 4 + 1)) << 16;
   }
+  const uint32_t v[4] = {value_pair<0>(w, scale), value_pair<1>(w, scale), value_pair<2>(w, scale),
+                         value_pair<3>(w, scale)};
+  store8_pairs<kStream>((value ? vc : kc) + ((size_t)bh * n_rows + row) * D + e, v);
 }
 
 struct AppendArgs {
@@ -118,24 +120,29 @@ struct AppendArgs {
   uint8_t* cache;
   const int32_t* res_len;
   int32_t* main_len;
-  int n_new, Hkv, C, Rcap;
+  int n_new, C, Rcap;
 };
 
-// One block per (b, kv head), a wave per row: keys and values of token 0, of
-// token 1, ...
-template <typename T, int D>
+// A wave per row (keys and values of a token are two); a block has kTokens tokens
+// of one (b, kv head). kAdvance: the block has all of the call's tokens and
+// advances main_len itself; else advance_kernel does, once every block has read it.
+constexpr int kTokens = 8;
+
+template <typename T, int D, bool kAdvance>
 __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
   using Q = QuantBlock<D>;
-  const int bh = blockIdx.x, b = bh / a.Hkv, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int bh = blockIdx.z * gridDim.y + blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   int r, n;
   cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
   const int want = a.n_tok ? clampi(a.n_tok[b], 0, a.n_new) : a.n_new;
   const int take = min(want, a.C - r - n);
+  const int t0 = blockIdx.x * kTokens, rows = 2 * min(kTokens, take - t0);
   uint8_t* head = a.cache + (size_t)bh * ((a.C + 63) / 64) * Q::kBytes;
   const int l = min(lane, D / 2 - 1);  // lanes past the row do its last pair again and store nothing
   __shared__ double2 s_cs[kThreads / 64][64];
-  for (int row = wave; row < 2 * take; row += kThreads / 64) {  // wave-uniform
-    const int t = row >> 1;
+  for (int row = wave; row < rows; row += kThreads / 64) {  // wave-uniform
+    const int t = t0 + (row >> 1);
     const bool value = row & 1;
     const T* src = static_cast<const T*>(value ? a.v_new : a.k_new) + ((size_t)bh * a.n_new + t) * D;
     const PairIndex at(!value && a.positions ? a.rope.rot_dim : 0, a.rope.layout);
@@ -143,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
     x.load(src, 2 * l, at);
     y.load(src, 2 * l + 1, at);
     if (at.rot) {
-      if (lane < a.rope.rot_dim / 2)
+      if (lane < at.rot / 2)
         s_cs[wave][lane] = turn(a.rope.freq[lane], a.positions[(size_t)b * a.n_new + t], a.rope.attn_scale);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -153,8 +160,20 @@ __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
                        x.rotated(2 * l, at, s_cs[wave]), y.rotated(2 * l + 1, at, s_cs[wave]), lane);
     __builtin_amdgcn_wave_barrier();
   }
-  __syncthreads();  // every wave has read the lengths
-  if (tid == 0 && take > 0) a.main_len[bh] = n + take;
+  if (kAdvance) {
+    __syncthreads();  // every wave has read the lengths
+    if (tid == 0 && take > 0) a.main_len[bh] = n + take;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void advance_kernel(AppendArgs a, int BH, int Hkv) {
+  const int bh = blockIdx.x * kThreads + threadIdx.x;
+  if (bh >= BH) return;
+  int r, n;
+  cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
+  const int want = a.n_tok ? clampi(a.n_tok[bh / Hkv], 0, a.n_new) : a.n_new;
+  const int take = min(want, a.C - r - n);
+  if (take > 0) a.main_len[bh] = n + take;
 }
 
 unsigned blocks_for(long long threads) { return (unsigned)((threads + kThreads - 1) / kThreads); }
@@ -162,23 +181,31 @@ unsigned blocks_for(long long threads) { return (unsigned)((threads + kThreads -
 template <typename T, int D>
 void launch_pack(const reskv_shape_t& s, const void* kc, const void* vc, const int32_t* res_len,
                  const int32_t* main_len, void* cache, hipStream_t stream) {
-  const int BH = s.batch * s.num_kv_heads;
-  hipLaunchKernelGGL((pack_kernel<T, D>), dim3(blocks_for(2LL * BH * s.slot_cap * (D / 32))), dim3(kThreads), 0, stream,
-                     (const T*)kc, (const T*)vc, res_len, main_len, (uint8_t*)cache, BH, s.slot_cap, s.res_cap);
+  hipLaunchKernelGGL((pack_kernel<T, D>), dim3(blocks_for(((long long)s.slot_cap * (D / 8) + kUnroll - 1) / kUnroll), 2 * s.num_kv_heads, s.batch),
+                     dim3(kThreads), 0, stream, (const T*)kc, (const T*)vc, res_len, main_len, (uint8_t*)cache,
+                     s.num_kv_heads, s.slot_cap, s.res_cap);
 }
 
 template <typename T, int D>
 void launch_unpack(const reskv_shape_t& s, const void* cache, const int32_t* res_len, const int32_t* main_len,
                    const int32_t* first, int n_rows, void* kc, void* vc, hipStream_t stream) {
-  const int BH = s.batch * s.num_kv_heads;
-  hipLaunchKernelGGL((unpack_kernel<T, D>), dim3(blocks_for(2LL * BH * n_rows * (D / 32))), dim3(kThreads), 0, stream,
-                     (const uint8_t*)cache, res_len, main_len, first, n_rows, (T*)kc, (T*)vc, BH, s.slot_cap,
-                     s.res_cap);
+  const dim3 grid(blocks_for((long long)n_rows * (D / 8)), 2 * s.num_kv_heads, s.batch);
+  const bool past = 2.0 * sizeof(T) * s.batch * s.num_kv_heads * n_rows * D > kStreamBytes;
+  auto kernel = past ? unpack_kernel<T, D, true> : unpack_kernel<T, D, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, (const uint8_t*)cache, res_len, main_len, first, n_rows,
+                     (T*)kc, (T*)vc, s.num_kv_heads, s.slot_cap, s.res_cap);
 }
 
 template <typename T, int D>
-void launch_append(const AppendArgs& aa, int BH, hipStream_t stream) {
-  hipLaunchKernelGGL((append_quant_kernel<T, D>), dim3(BH), dim3(kThreads), 0, stream, aa);
+void launch_append(const reskv_shape_t& s, const AppendArgs& aa, hipStream_t stream) {
+  const dim3 grid((aa.n_new + kTokens - 1) / kTokens, s.num_kv_heads, s.batch);
+  if (grid.x == 1) {
+    hipLaunchKernelGGL((append_quant_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, aa);
+    return;
+  }
+  hipLaunchKernelGGL((append_quant_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, aa);
+  const int BH = s.batch * s.num_kv_heads;
+  hipLaunchKernelGGL(advance_kernel, dim3(blocks_for(BH)), dim3(kThreads), 0, stream, aa, BH, s.num_kv_heads);
 }
 
 }  // namespace
@@ -220,11 +247,10 @@ hipError_t launch_append_quant(const reskv_shape_t& s, const reskv_rope_t* rope,
   aa.positions = rope ? positions : nullptr;
   aa.n_tok = n_tok; aa.k_new = k_new; aa.v_new = v_new; aa.cache = (uint8_t*)cache;
   aa.res_len = res_len; aa.main_len = main_len;
-  aa.n_new = n_new; aa.Hkv = s.num_kv_heads; aa.C = s.slot_cap; aa.Rcap = s.res_cap;
+  aa.n_new = n_new; aa.C = s.slot_cap; aa.Rcap = s.res_cap;
   const bool bf = s.dtype == RESKV_BF16;
-  const int BH = s.batch * s.num_kv_heads;
-  if (s.head_dim == 128) bf ? launch_append<uint16_t, 128>(aa, BH, stream) : launch_append<float, 128>(aa, BH, stream);
-  else bf ? launch_append<uint16_t, 64>(aa, BH, stream) : launch_append<float, 64>(aa, BH, stream);
+  if (s.head_dim == 128) bf ? launch_append<uint16_t, 128>(s, aa, stream) : launch_append<float, 128>(s, aa, stream);
+  else bf ? launch_append<uint16_t, 64>(s, aa, stream) : launch_append<float, 64>(s, aa, stream);
   return hipGetLastError();
 }
 
