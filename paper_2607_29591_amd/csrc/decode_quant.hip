@@ -551,57 +551,62 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
   if (!kSplit && app && tid == 0) a.main_len[bh] = n;
 }
 
-// Join the records of one query head: one block of D threads, thread d a column.
-// Every record has its maximum and sum (those without slots -inf and 0), so the
-// cache lengths are not read, and main_len advances here: by the block of the
-// group's first head, which alone reads it.
+// Join the records of one query head: thread = one column (tid % D) of every
+// kGroups-th part. Outputs are requested before their weights are known; every
+// record has its maximum and sum (those without slots -inf and 0: what is read of
+// their outputs does not enter), so the cache lengths are not needed, and main_len
+// advances here: by the block of the group's first head, which alone reads it.
+constexpr int kJoinThreads = 512;
+
 template <int D, int GP>
-__global__ __launch_bounds__(D) void decode_quant_combine(QuantDecodeArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void decode_quant_combine(QuantDecodeArgs a) {
+  constexpr int kGroups = kJoinThreads / D, kPer = kMaxParts / kGroups;  // parts of a thread
   const int h = blockIdx.x, bh = blockIdx.z * gridDim.y + blockIdx.y;
-  const int d = threadIdx.x, lane = d & 63;
-  __shared__ float s_w[2 * kMaxParts];
-  const size_t row0 = (size_t)bh * a.P * 2 * GP + h;  // record i = 2 p + kind is row i GP further
+  const int tid = threadIdx.x, lane = tid & 63, d = tid % D, group = tid / D;
+  __shared__ float s_w[2][kMaxParts];
+  __shared__ float s_o[kGroups][D];
+  const size_t row0 = (size_t)bh * a.P * 2 * GP + h;  // record (part p, kind) is row (2 p + kind) GP further
   const float2* ml = reinterpret_cast<const float2*>(a.rec_ml) + row0;
-  constexpr int kPer = 2 * kMaxParts / 64;
-  const bool is_main = lane & 1;  // a lane's records are all of one kind
-  float2 e[kPer];
-  float own = kNegInf;
+  const int P = a.P, mine = min(lane, P - 1);
+  float2 eR = ml[(size_t)(2 * mine) * GP], eM = ml[(size_t)(2 * mine + 1) * GP];
+  const float* acc = a.rec_acc + row0 * D + d;
+  float vR[kPer], vM[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const int i = lane + 64 * k;
-    e[k] = i < 2 * a.P ? ml[(size_t)i * GP] : make_float2(kNegInf, 0.f);
-    own = fmaxf(own, e[k].x);
+    const int p = min(group + k * kGroups, P - 1);
+    vR[k] = acc[(size_t)(2 * p) * GP * D];
+    vM[k] = acc[(size_t)(2 * p + 1) * GP * D];
   }
-#pragma unroll
-  for (int x = 2; x < 64; x <<= 1) own = wave_xor_max(own, x);
-  float sum = 0.f;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (e[k].x != kNegInf) sum = fmaf(e[k].y, exp2f(e[k].x - own), sum);
-#pragma unroll
-  for (int x = 2; x < 64; x <<= 1) sum = wave_xor_add(sum, x);
-  const float mR = __shfl(own, 0, 64), mM = __shfl(own, 1, 64), lR = __shfl(sum, 0, 64), lM = __shfl(sum, 1, 64);
+  if (lane >= P) eR = eM = make_float2(kNegInf, 0.f);
+  const float mR = rows4_max(row16_max(eR.x)), mM = rows4_max(row16_max(eM.x));
+  const float fR = eR.x != kNegInf ? exp2f(eR.x - mR) : 0.f, fM = eM.x != kNegInf ? exp2f(eM.x - mM) : 0.f;
+  const float lR = rows4_sum(row16_sum(eR.x != kNegInf ? fR * eR.y : 0.f));
+  const float lM = rows4_sum(row16_sum(eM.x != kNegInf ? fM * eM.y : 0.f));
   const int qh = bh * a.G + h;
   const Joined j = join(a, qh, mM, lM, mR, lR);
-  if (d < 64) {
-#pragma unroll
-    for (int k = 0; k < kPer; ++k)  // -1: a record without slots, whose outputs were not written
-      s_w[lane + 64 * k] = e[k].x != kNegInf ? exp2f(e[k].x - own) * (is_main ? j.fM : j.fR) * j.inv : -1.f;
+  if (tid < 64) {  // -1: a record without slots
+    s_w[0][lane] = eR.x != kNegInf ? fR * j.fR * j.inv : -1.f;
+    s_w[1][lane] = eM.x != kNegInf ? fM * j.fM * j.inv : -1.f;
   }
   __syncthreads();
-  const float* acc = a.rec_acc + row0 * D + d;
   float o = 0.f;
-  for (int i0 = 0; i0 < 2 * a.P; i0 += 8) {
-    float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      v[k] = i0 + k < 2 * a.P && !(s_w[i0 + k] < 0.f) ? acc[(size_t)(i0 + k) * GP * D] : 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (i0 + k < 2 * a.P && !(s_w[i0 + k] < 0.f)) o = fmaf(s_w[i0 + k], v[k], o);
+  for (int k = 0; k < kPer; ++k) {
+    const int p = group + k * kGroups;
+    if (p >= P) continue;
+    const float wR = s_w[0][p], wM = s_w[1][p];
+    if (!(wR < 0.f)) o = fmaf(wR, vR[k], o);
+    if (!(wM < 0.f)) o = fmaf(wM, vM[k], o);
   }
-  a.out[(size_t)qh * D + d] = o;
-  if (d == 0) {
+  s_o[group][d] = o;
+  __syncthreads();
+  if (group == 0) {
+    o = s_o[0][d];
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) o += s_o[g][d];
+    a.out[(size_t)qh * D + d] = o;
+  }
+  if (tid == 0) {
     write_stats(a, qh, mM, lM, mR, lR, j.gate);
     if (h == 0 && a.k_new) {
       int r, n;
@@ -618,7 +623,7 @@ void launch_kernels(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStr
     return;
   }
   hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.Hkv, pl.B, pl.P), dim3(kThreads), 0, stream, da);
-  hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(da.G, pl.Hkv, pl.B), dim3(D), 0, stream, da);
+  hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(da.G, pl.Hkv, pl.B), dim3(kJoinThreads), 0, stream, da);
 }
 
 template <typename T, int D>
