@@ -27,6 +27,9 @@ namespace reskv {
 
 namespace {
 
+// Two waves a SIMD. 16 waves of half the registers and units ran 23.6 us where 8 run
+// 17.3 (256 heads of 2048 slots): what a wave does once weighs as much as two units.
+// Requesting a unit ahead changed nothing (17.4).
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kUnit = 64;  // slots of a cache block
@@ -104,21 +107,23 @@ __device__ __forceinline__ float byte_scale(uint32_t w) {
   return scale_of((w >> (8 * kByte)) & 0xffu);
 }
 
-// A row fragment: elements g D/4 .. (g + 1) D/4 of one row as bf16 pairs, D / 32
-// matrix steps of 8 elements.
-template <int D>
-struct Row {
-  uint4 s[D / 32];
-};
-
 // 8 codes of a word as 8 bf16 numbers.
 __device__ __forceinline__ uint4 eight(uint32_t codes, float scale) {
   return make_uint4(value_pair<0>(codes, scale), value_pair<1>(codes, scale), value_pair<2>(codes, scale),
                     value_pair<3>(codes, scale));
 }
 
-template <int D, int NP>
-__device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[NP], float (&s)[kTiles][4]) {
+// Products of the unit's keys and the queries, whose fragments are read from LDS
+// here (kept in registers over the unit they would not fit beside the rest).
+template <int D, int GP, int NP>
+__device__ __forceinline__ void unit_logits(const Unit<D>& u, const uint16_t (*s_q)[GP][D], int hq, int g,
+                                            float (&s)[kTiles][4]) {
+  uint4 q[NP][D / 32];
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      q[p][i] = *reinterpret_cast<const uint4*>(&s_q[p][min(hq, GP - 1)][g * (D / 4) + 8 * i]);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const float scale = t == 0 ? byte_scale<0>(u.ks) : t == 1 ? byte_scale<1>(u.ks)
@@ -129,7 +134,7 @@ __device__ __forceinline__ void unit_logits(const Unit<D>& u, const Row<D> (&q)[
       const bf16x8_t k = as_bf16x8(eight(u.k[t].w[i], scale));
 #pragma unroll
       for (int p = NP - 1; p >= 0; --p)  // the smallest part first
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16x8(q[p].s[i]), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16x8(q[p][i]), c, 0, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[t][i] = c[i];
@@ -164,8 +169,7 @@ constexpr bool kPaired = GP <= 8;
 
 // O^T += V^T P^T for the unit; rows without weight must hold finite numbers.
 template <int D, int GP>
-__device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const float (&vs)[kTiles][4],
-                                        const float (&p)[kTiles][4], int hd) {
+__device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const float (&p)[kTiles][4], int hd) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t bh[4], bl[4];
@@ -191,12 +195,20 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
         if (!kPaired<GP>) st.acc[e + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, Bl, st.acc[e + o], 0, 0, 0);
       }
     };
+    float vs[8];  // scales of the rows
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      vs[4 * t] = byte_scale<0>(u.vs.w[2 * h + t]);
+      vs[4 * t + 1] = byte_scale<1>(u.vs.w[2 * h + t]);
+      vs[4 * t + 2] = byte_scale<2>(u.vs.w[2 * h + t]);
+      vs[4 * t + 3] = byte_scale<3>(u.vs.w[2 * h + t]);
+    }
     uint32_t x[8];
     if constexpr (D == 128) {  // a word per row
 #define RESKV_PAIRS(B)                                                                       \
   {                                                                                          \
     _Pragma("unroll") for (int k = 0; k < 8; ++k) x[k] =                                     \
-        value_pair<B>(u.v[2 * h + k / 4].w[k % 4], vs[2 * h + k / 4][k % 4]);                \
+        value_pair<B>(u.v[2 * h + k / 4].w[k % 4], vs[k]);                                   \
     step(2 * B, x);                                                                          \
   }
       RESKV_PAIRS(0) RESKV_PAIRS(1) RESKV_PAIRS(2) RESKV_PAIRS(3)
@@ -205,8 +217,8 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
 #define RESKV_PAIRS(B)                                                                       \
   {                                                                                          \
     _Pragma("unroll") for (int k = 0; k < 8; k += 2) {                                       \
-      x[k] = value_pair<B>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[2 * h + k / 4][k % 4]);       \
-      x[k + 1] = value_pair<B + 2>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[2 * h + k / 4][k % 4 + 1]); \
+      x[k] = value_pair<B>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[k]);                          \
+      x[k + 1] = value_pair<B + 2>(u.v[2 * h + k / 4].w[k % 4 / 2], vs[k + 1]);              \
     }                                                                                        \
     step(2 * B, x);                                                                          \
   }
@@ -217,64 +229,52 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
 }
 
 // Online softmax over the unit's slots [lo, hi) of one kind, from the logits'
-// products s. Residual slots add beta * log2 count; slots of no weight (outside,
-// empty entries) get zero probability and a zero scale, so whatever their codes
-// say does not enter. A unit full of main slots needs none of that.
+// products p, which become the probabilities. Residual slots add beta * log2 count;
+// slots of no weight (outside, empty entries) get zero probability and the least
+// scale, so whatever their codes say does not enter. A unit full of main slots
+// needs none of that.
 template <int D, int GP>
-__device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const float (&s)[kTiles][4],
-                                           int lo, int hi, bool is_res, float qk_scale, float beta_log2, float* s_bias,
-                                           int lane) {
+__device__ __forceinline__ void softmax_pv(State<D>& st, Unit<D>& u, float (&p)[kTiles][4], int lo, int hi,
+                                           bool is_res, float qk_scale, float beta_log2, float* s_bias, int lane) {
   const int hd = lane & 15, g = lane >> 4;
-  float p[kTiles][4], vs[kTiles][4];
-  float top = kNegInf, m_new, mu;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    vs[t][0] = byte_scale<0>(u.vs.w[t]);
-    vs[t][1] = byte_scale<1>(u.vs.w[t]);
-    vs[t][2] = byte_scale<2>(u.vs.w[t]);
-    vs[t][3] = byte_scale<3>(u.vs.w[t]);
-  }
-  if (!is_res && lo <= 0 && hi >= kUnit) {  // wave-uniform
+  float top = kNegInf;
+  const bool full = !is_res && lo <= 0 && hi >= kUnit;  // wave-uniform
+  if (full) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-    m_new = fmaxf(st.m, rows4_max(top) * qk_scale);
-    mu = m_new == kNegInf ? 0.f : m_new;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(fmaf(s[t][i], qk_scale, -mu));
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, p[t][i]);
+    top *= qk_scale;
   } else {
     // what a slot's logits are moved by (-inf: no weight), from the lane of the
     // slot to the lanes of its logits
     const bool weighs = lane >= lo && lane < hi && !(is_res && u.lc == kNegInf);
     s_bias[lane] = !weighs ? kNegInf : is_res ? beta_log2 * u.lc : 0.f;
-    f32x4_t bias[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) bias[t] = *reinterpret_cast<const f32x4_t*>(&s_bias[16 * t + 4 * g]);
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int t = 0; t < kTiles; ++t) {
+      const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(&s_bias[16 * t + 4 * g]);
+      uint32_t mask = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool live = bias[t][i] != kNegInf;
-        p[t][i] = live ? fmaf(s[t][i], qk_scale, bias[t][i]) : kNegInf;
-        vs[t][i] = live ? vs[t][i] : 0.f;
+        const bool live = bias[i] != kNegInf;
+        p[t][i] = live ? fmaf(p[t][i], qk_scale, bias[i]) : kNegInf;
+        mask |= live ? 0xffu << (8 * i) : 0u;
         top = fmaxf(top, p[t][i]);
       }
-    m_new = fmaxf(st.m, rows4_max(top));
-    mu = m_new == kNegInf ? 0.f : m_new;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[t][i] = fast_exp2(p[t][i] - mu);
+      u.vs.w[t] &= mask;
+    }
   }
+  const float m_new = fmaxf(st.m, rows4_max(top));
+  const float mu = m_new == kNegInf ? 0.f : m_new, scale = full ? qk_scale : 1.f;
   const float alpha = fast_exp2(st.m - mu);
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += p[t][i];
+    for (int i = 0; i < 4; ++i) {
+      p[t][i] = fast_exp2(fmaf(p[t][i], scale, -mu));
+      sum += p[t][i];
+    }
   sum = rows4_sum(sum);
   st.l = fmaf(st.l, alpha, sum);
   // logits that are all NaN leave no maximum: 0 in its place keeps their sum in the merges
@@ -283,7 +283,7 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, const Unit<D>& u, const
   for (int e = 0; e < State<D>::kE; ++e)
 #pragma unroll
     for (int i = 0; i < 4; ++i) st.acc[e][i] *= alpha;
-  pv_unit<D, GP>(st, u, vs, p, hd);
+  pv_unit<D, GP>(st, u, p, hd);
 }
 
 template <int D, int GP>
@@ -343,7 +343,6 @@ template <typename T, int D, int GP, bool kSplit>
 __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs a) {
   using Q = QuantBlock<D>;
   constexpr int NP = sizeof(T) == 2 ? 1 : 3;
-  constexpr bool kAhead = NP == 1 || D == 64;  // registers for a second unit
   const int kvh = blockIdx.x, b = blockIdx.y, part = kSplit ? blockIdx.z : 0;
   const int bh = b * gridDim.x + kvh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -436,49 +435,38 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
     store_row_quant<D>(cache + (size_t)app_blk * Q::kBytes, app_slot % kUnit, wave == 1,
                        ne[0].rotated(2 * l_new, at_new, s_cs), ne[1].rotated(2 * l_new + 1, at_new, s_cs), lane);
   __syncthreads();
-  Row<D> q[NP];
   const int hq = kPaired<GP> ? hd & 7 : hd;  // query head of this lane's column
-#pragma unroll
-  for (int p = 0; p < NP; ++p)
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-      q[p].s[i] = hq < GP ? *reinterpret_cast<const uint4*>(&s_q[p][hq][g * (D / 4) + 8 * i]) : make_uint4(0, 0, 0, 0);
   if (app_blk == begin + wave) u.load(cache, app_blk, logc, Rcap, lane);  // with the new token
 
-  // The waves take the cache blocks in turn, the next one requested before the
-  // present one is worked on; residual slots come first, and the block that holds
-  // slot r has a part of each kind.
+  // Units: the cache blocks in order (their residual slots if they have any), then
+  // once more the one that holds slot r, for its main slots. The waves take them in
+  // turn, so each meets its residual units first.
   State<D> st;
   st.reset();
   bool in_res = true;
-  auto work = [&](const Unit<D>& u, int blk) __attribute__((always_inline)) {
-    const int s0 = blk * kUnit;
-    float s[kTiles][4];
-    unit_logits<D, NP>(u, q, s);
-    const int last = s0 + kUnit > r ? 1 : 0;
-    for (int kind = s0 < r ? 0 : 1; kind <= last; ++kind) {
-      if (kind == 1 && in_res) {
-        store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
-        st.reset();
-        in_res = false;
-      }
-      softmax_pv<D, GP>(st, u, s, kind ? r - s0 : 0, (kind ? total : r) - s0, kind == 0, a.qk_scale, a.beta_log2,
-                        s_bias[wave], lane);
+  const bool both = r % kUnit != 0 && n > 0 && r / kUnit >= begin && r / kUnit < end;
+  const int units = end - begin + (both ? 1 : 0);
+  auto block_of = [&](int i) { return i < end - begin ? begin + i : r / kUnit; };
+  auto work = [&](Unit<D>& u, int i) __attribute__((always_inline)) {
+    const int s0 = block_of(i) * kUnit;
+    const bool is_res = i < end - begin && s0 < r;
+    if (!is_res && in_res) {
+      store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
+      st.reset();
+      in_res = false;
     }
+    float p[kTiles][4];
+    unit_logits<D, GP, NP>(u, s_q, hq, g, p);
+    softmax_pv<D, GP>(st, u, p, is_res ? 0 : r - s0, (is_res ? r : total) - s0, is_res, a.qk_scale, a.beta_log2,
+                      s_bias[wave], lane);
   };
-  int blk = begin + wave;
-  for (; blk + kWaves < end; blk += kWaves) {
-    if constexpr (kAhead) {
-      Unit<D> next;
-      next.load(cache, blk + kWaves, logc, Rcap, lane);
-      work(u, blk);
-      u = next;
-    } else {
-      work(u, blk);
-      u.load(cache, blk + kWaves, logc, Rcap, lane);
-    }
+  int i = wave;
+  if (both && i == units - 1) u.load(cache, r / kUnit, logc, Rcap, lane);
+  for (; i + kWaves < units; i += kWaves) {
+    work(u, i);
+    u.load(cache, block_of(i + kWaves), logc, Rcap, lane);
   }
-  if (blk < end) work(u, blk);  // on its own: nothing more to request or to wait for
+  if (i < units) work(u, i);
   if (in_res) {
     store_state<D, GP>(st, s_acc[0][wave], s_m[0][wave], s_l[0][wave], hd, g);
     st.reset();
@@ -514,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
       if (h < G) {
         const int qh = bh * G + h;
         const Joined j = join(a, qh, mM, lM, mR, lR);
-        s_w[kind][w][h] = f * (kind ? j.fM : j.fR) * j.inv;
+        s_w[kind][w][h] = m != kNegInf ? f * (kind ? j.fM : j.fR) * j.inv : 0.f;
         if ((tid & 15) == 0) write_stats(a, qh, mM, lM, mR, lR, j.gate);
       }
     }
@@ -619,10 +607,12 @@ __global__ __launch_bounds__(kJoinThreads) void decode_quant_combine(QuantDecode
 template <typename T, int D, int GP>
 void launch_kernels(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipStream_t stream) {
   if (pl.P == 1) {
-    hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, false>), dim3(pl.Hkv, pl.B), dim3(kThreads), 0, stream, da);
+    hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, false>), dim3(pl.Hkv, pl.B), dim3(kThreads), 0,
+                       stream, da);
     return;
   }
-  hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.Hkv, pl.B, pl.P), dim3(kThreads), 0, stream, da);
+  hipLaunchKernelGGL((decode_quant_kernel<T, D, GP, true>), dim3(pl.Hkv, pl.B, pl.P), dim3(kThreads), 0,
+                     stream, da);
   hipLaunchKernelGGL((decode_quant_combine<D, GP>), dim3(da.G, pl.Hkv, pl.B), dim3(kJoinThreads), 0, stream, da);
 }
 
