@@ -357,6 +357,7 @@ static reskv_status_t check_quant_shape(const reskv_shape_t* s) {
   if (st != RESKV_OK) return st;
   if (s->batch > 65535 || s->num_kv_heads > 32767)
     return fail(RESKV_ERR_UNSUPPORTED, "batch %d above 65535 or %d KV heads above 32767", s->batch, s->num_kv_heads);
+  if (s->slot_cap > 1 << 30) return fail(RESKV_ERR_UNSUPPORTED, "slot_cap %d above 2^30", s->slot_cap);
   return RESKV_OK;
 }
 
@@ -419,6 +420,10 @@ reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rop
 
 size_t reskv_decode_quant_workspace_size(const reskv_shape_t* shape) {
   return check_quant_shape(shape) == RESKV_OK ? make_quant_decode_plan(*shape).bytes : 0;
+}
+
+int reskv_internal_quant_parts(const reskv_shape_t* shape) {
+  return check_quant_shape(shape) == RESKV_OK ? make_quant_decode_plan(*shape).P : -1;
 }
 
 reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_gate_t* gate, const reskv_rope_t* rope,

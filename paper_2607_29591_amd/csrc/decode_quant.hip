@@ -630,6 +630,22 @@ hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipSt
 
 }  // namespace
 
+// One block per (b, kv head), or its cache blocks dealt to several and their records
+// joined by a second launch. A block takes 512 slots a round (8 waves of 64), about
+// 2 us each while the blocks do not fill the memory's rate; the join and its launch
+// cost 3 us, more once 256 blocks stream at once. Blocks past 256 (one a CU) only
+// wait. Measured at d = 128, bf16, 4 query heads per KV head, every slot live, us one
+// block / split so that up to 256 blocks run (lengths uniform in [C/4, C] within 1 us
+// of both):
+//   pairs     C = 1024     1500       2048       2560       4096       8192
+//     1      8.6/ 9.7  10.7/ 9.6  12.6/ 9.6  14.5/ 9.7  20.1/ 9.9  35.3/ 9.9
+//    32      8.9/10.0  11.0/10.2  13.0/10.3  15.5/10.8  21.6/12.0  37.9/14.5
+//    64      9.1/10.3  11.7/11.4  13.6/12.0  15.7/13.6  22.0/14.4  38.2/19.6
+//   128     10.0/12.9  12.2/14.9  14.5/15.2  16.3/19.2  22.5/20.6  46.1/35.2
+//   240     11.0/20.4  14.2/22.6  16.7/25.1  18.9/27.6  30.6/38.1  (two or more each)
+// (8 query heads 0.5 to 1 us more on both sides; fp32 rows of 64, 32 pairs: 7.6/8.3,
+// 9.3/8.4, 10.8/8.3, 12.2/8.6, 17.3/8.6, 31.9/11.2.) So a split has to save two
+// rounds, four where the pairs alone fill more than a quarter of the CUs.
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   QuantDecodePlan p{};
   p.B = s.batch;
@@ -637,14 +653,16 @@ QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   const long long BH = (long long)p.B * p.Hkv;
   const int G = s.num_q_heads / s.num_kv_heads;
   p.GP = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : G <= 8 ? 8 : 16;
-  const int NB = (s.slot_cap + kUnit - 1) / kUnit;
+  const int NB = (int)(((long long)s.slot_cap + kUnit - 1) / kUnit);
   p.P = 1;
   p.W = NB;
-  if (BH < 256 && NB > 2 * kWaves) {
+  if (BH <= 128) {
     const int want = 256 / (int)BH < kMaxParts ? 256 / (int)BH : kMaxParts;
-    p.W = (NB + want - 1) / want;
-    p.W = (p.W + kWaves - 1) / kWaves * kWaves;
-    p.P = (NB + p.W - 1) / p.W;
+    const int rounds = (NB + kWaves - 1) / kWaves, each = (rounds + want - 1) / want;
+    if (rounds - each >= (BH <= 64 ? 2 : 4)) {
+      p.W = each * kWaves;
+      p.P = (NB + p.W - 1) / p.W;
+    }
   }
   const size_t rows = p.P > 1 ? (size_t)BH * p.P * 2 * p.GP : 0;
   p.acc_off = align_up(rows * 2 * sizeof(float), 256);
@@ -668,7 +686,7 @@ hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, co
   da.P = pl.P; da.W = pl.W;
   da.dbg_lse_main = dbg_lse_main; da.dbg_lse_res = dbg_lse_res; da.dbg_gate = dbg_gate;
   da.G = s.num_q_heads / s.num_kv_heads;
-  da.C = s.slot_cap; da.Rcap = s.res_cap; da.NB = (s.slot_cap + kUnit - 1) / kUnit;
+  da.C = s.slot_cap; da.Rcap = s.res_cap; da.NB = (int)(((long long)s.slot_cap + kUnit - 1) / kUnit);
   da.qk_scale = kLog2e / sqrtf((float)s.head_dim);
   da.beta_log2 = g.beta * kLog2e;
   da.tau_scalar = g.tau_scalar; da.alpha = g.alpha; da.g_min = g.g_min;

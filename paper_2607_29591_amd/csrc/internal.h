@@ -89,6 +89,9 @@ struct QuantDecodePlan {
   size_t acc_off, bytes;
 };
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s);
+// Blocks a (b, kv head) is split over in a 4-bit decode of these sizes, for the
+// tests (not part of the C ABI); -1 where the call is refused.
+extern "C" int reskv_internal_quant_parts(const reskv_shape_t* shape);
 hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, const QuantDecodePlan& pl,
                                const reskv_rope_t* rope, const int32_t* positions, const void* q, void* cache,
                                const float* logc, const int32_t* res_len, int32_t* main_len, const void* k_new,

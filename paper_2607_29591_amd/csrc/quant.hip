@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const T* kc, const T* vc
   cache_lengths(res_len, main_len, bh, C, Rcap, r, n);
   if (first >= r + n) return;  // the four lanes of a group alike
   const T* src = (value ? vc : kc) + (size_t)bh * C * D + e;
-  uint8_t* head = cache + (size_t)bh * ((C + 63) / 64) * Q::kBytes;
+  uint8_t* head = cache + (size_t)bh * (((size_t)C + 63) / 64) * Q::kBytes;
   float x[kUnroll][8];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) load8_f32(src + min(first + u * kSlots, (long long)(r + n - 1)) * D, x[u]);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t* cache, 
   cache_lengths(res_len, main_len, bh, C, Rcap, r, n);
   const long long slot = (first ? first[bh] : 0) + row;
   if (row >= n_rows || slot < 0 || slot >= r + n) return;
-  const uint8_t* block = cache + ((size_t)bh * ((C + 63) / 64) + slot / 64) * Q::kBytes;
+  const uint8_t* block = cache + ((size_t)bh * (((size_t)C + 63) / 64) + slot / 64) * Q::kBytes;
   const int s = (int)(slot % 64);
   const float scale = scale_of(block[value ? Q::v_scale(s, e / 32) : Q::k_scale(s, e / 32)]);
   uint32_t w;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
   const int want = a.n_tok ? clampi(a.n_tok[b], 0, a.n_new) : a.n_new;
   const int take = min(want, a.C - r - n);
   const int t0 = blockIdx.x * kTokens, rows = 2 * min(kTokens, take - t0);
-  uint8_t* head = a.cache + (size_t)bh * ((a.C + 63) / 64) * Q::kBytes;
+  uint8_t* head = a.cache + (size_t)bh * (((size_t)a.C + 63) / 64) * Q::kBytes;
   const int l = min(lane, D / 2 - 1);  // lanes past the row do its last pair again and store nothing
   __shared__ double2 s_cs[kThreads / 64][64];
   for (int row = wave; row < rows; row += kThreads / 64) {  // wave-uniform
@@ -211,7 +211,7 @@ void launch_append(const reskv_shape_t& s, const AppendArgs& aa, hipStream_t str
 }  // namespace
 
 size_t quant_cache_bytes(const reskv_shape_t& s) {
-  return (size_t)s.batch * s.num_kv_heads * ((s.slot_cap + 63) / 64) * 68 * s.head_dim;
+  return (size_t)s.batch * s.num_kv_heads * (((size_t)s.slot_cap + 63) / 64) * 68 * s.head_dim;
 }
 
 hipError_t launch_pack_quant(const reskv_shape_t& s, const void* kc, const void* vc, const int32_t* res_len,

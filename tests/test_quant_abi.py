@@ -61,6 +61,17 @@ def test_sizes():
     assert rk.reskv_quant_cache_size(shape()) * 8 == 4.25 * 2 * 2 * 640 * 2 * 128
 
 
+@pytest.mark.parametrize("pairs,cap,parts", [
+    (8, 1024, 1), (8, 1025, 3), (1, 512, 1), (1, 65536, 64), (1, 1 << 20, 64), (64, 1024, 1), (64, 1536, 3),
+    (64, 2560, 3), (65, 2048, 1), (128, 3500, 1), (128, 4096, 2), (128, 8192, 2), (129, 8192, 1), (256, 65536, 1)])
+def test_when_a_head_is_split(pairs, cap, parts):
+    """A split that saves two rounds of 512 slots (four from 65 pairs on), over up to 256 blocks."""
+    s = rk.make_shape(pairs, 4, 1, 128, "bf16", cap, 8)
+    assert rk.lib().reskv_internal_quant_parts(ctypes.byref(s)) == parts
+    records = 2 * pairs * parts * 4 * (128 + 2) * 4 if parts > 1 else 0
+    assert records <= rk.reskv_decode_quant_workspace_size(s) <= records + 1024
+
+
 def rope_call(s=None, plan=None, n=5, pos=P, q=P, qs=(5120, 640, 128), qo=P << 8, qos=(5120, 640, 128), k=None,
               ks=None, ko=None, kos=None):
     row = lambda x: None if x is None else ctypes.byref(rk.Rows(*x))  # noqa: E731
@@ -115,6 +126,8 @@ def quant_call(name, **kw):
 @pytest.mark.parametrize("name,kw,code", [
     (n, dict(s=shape(head_dim=96)), 2) for n in ("pack", "unpack", "append", "decode")] + [
     (n, dict(s=shape(slot_cap=0)), 1) for n in ("pack", "unpack", "append", "decode")] + [
+    (n, dict(s=shape(**x)), 2) for n in ("pack", "unpack", "append", "decode") for x in (
+        dict(batch=65536), dict(num_q_heads=32768, num_kv_heads=32768), dict(batch=1, slot_cap=(1 << 30) + 1))] + [
     (n, {x: None}, 1) for n in ("pack", "unpack", "append") for x in ("kc", "vc", "rl", "ml", "cache")] + [
     (n, {x: P + 4}, 1) for n in ("pack", "unpack", "append", "decode") for x in ("kc", "vc", "cache")] + [
     ("decode", {x: None}, 1) for x in ("q", "cache", "logc", "rl", "ml", "out", "kc", "vc", "gate")] + [

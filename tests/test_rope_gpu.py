@@ -137,6 +137,31 @@ def test_infinities_stay_in_their_pair():
     assert bad.nonzero().flatten().tolist() == [3, 35, 100]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_smallest_and_largest_numbers(dtype):
+    """Rows of subnormal numbers and of the largest ones: half a step of the result's binade, subnormal steps below
+    the normal range; results past the range are infinite."""
+    rng = np.random.default_rng(11)
+    x = torch.zeros(1, 3, 8, 64, dtype=DT[dtype], device="cuda")
+    tiny, big = torch.finfo(DT[dtype]).tiny, torch.finfo(DT[dtype]).max
+    step = tiny * torch.finfo(DT[dtype]).eps  # of the subnormal numbers
+    k = rng.integers(-100, 101, size=(8, 64))
+    x[0, 0] = torch.as_tensor(k.astype(np.float64) * step).to(torch.float32).to(DT[dtype])
+    x[0, 1] = torch.as_tensor(rng.uniform(-4, 4, size=(8, 64)) * tiny).to(torch.float32).to(DT[dtype])
+    x[0, 2] = torch.as_tensor(rng.uniform(-1, 1, size=(8, 64)) * big).to(torch.float32).to(DT[dtype])
+    pos = rng.integers(0, 5000, size=(1, 8)).astype(np.int32)
+    y = torch.zeros_like(x)
+    rk.reskv_rope(rk.make_shape(1, 3, 1, 64, dtype, 1, 1), rk.make_rope(64), torch.as_tensor(pos).cuda(), q=x, q_out=y)
+    want, atol = ref.rotate_atol(host(x), pos, 64, torch.finfo(DT[dtype]).eps)
+    atol = np.maximum(atol, 0.5 * step * (1 + 1e-6))
+    got = host(y)
+    edge = float(big) * (1 + torch.finfo(DT[dtype]).eps / 4)  # the middle between the largest number and infinity
+    fine = np.isfinite(got)
+    assert (np.abs(got - want)[fine] <= atol[fine]).all()
+    assert (np.abs(want[~fine]) >= edge * (1 - 1e-9)).all() and (np.abs(want[fine]) <= edge * (1 + 1e-9)).all()
+    assert (~fine).any() and fine[0, 0].all() and (got[0, 0] != 0).any()
+
+
 def test_graph_replays_and_streams():
     rng = np.random.default_rng(9)
     B, Hq, H, n = 4, 8, 2, 3
