@@ -320,11 +320,13 @@ __device__ __forceinline__ Joined join(const QuantDecodeArgs& a, int qh, float m
   const float pmax = lM > 0.f ? 1.f / lM : 1.f;
   Joined j;
   j.gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
-  const float lg = j.gate > 0.f ? log2f(j.gate) : kNegInf;
+  // hardware logarithm and powers (an ulp; the logarithm of a gate below 2^-126 by
+  // way of 2^64 of it, weights below 2^-126 are 0)
+  const float lg = j.gate > 0.f ? __builtin_amdgcn_logf(j.gate * 0x1p64f) - 64.f : kNegInf;
   const float mRg = (mR == kNegInf || lg == kNegInf) ? kNegInf : mR + lg;
   const float M = fmaxf(mM, mRg);
-  j.fM = mM != kNegInf ? exp2f(mM - M) : 0.f;
-  j.fR = mRg != kNegInf ? exp2f(mRg - M) : 0.f;
+  j.fM = mM != kNegInf ? fast_exp2(mM - M) : 0.f;
+  j.fR = mRg != kNegInf ? fast_exp2(mRg - M) : 0.f;
   const float den = lM * j.fM + lR * j.fR;
   j.inv = den != 0.f ? 1.f / den : 0.f;  // NaN stays NaN
   return j;
@@ -484,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
     M = fmaxf(M, dpp_move<0xB1>(M));
     M = fmaxf(M, dpp_move<0x4E>(M));
     M = fmaxf(M, dpp_move<0x141>(M));
-    const float f = m != kNegInf ? exp2f(m - M) : 0.f;
+    const float f = m != kNegInf ? fast_exp2(m - M) : 0.f;
     float L = m != kNegInf ? f * l : 0.f;
     L += dpp_move<0xB1>(L);
     L += dpp_move<0x4E>(L);
@@ -567,7 +569,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_quant_combine(QuantDecode
   }
   if (lane >= P) eR = eM = make_float2(kNegInf, 0.f);
   const float mR = rows4_max(row16_max(eR.x)), mM = rows4_max(row16_max(eM.x));
-  const float fR = eR.x != kNegInf ? exp2f(eR.x - mR) : 0.f, fM = eM.x != kNegInf ? exp2f(eM.x - mM) : 0.f;
+  const float fR = eR.x != kNegInf ? fast_exp2(eR.x - mR) : 0.f, fM = eM.x != kNegInf ? fast_exp2(eM.x - mM) : 0.f;
   const float lR = rows4_sum(row16_sum(eR.x != kNegInf ? fR * eR.y : 0.f));
   const float lM = rows4_sum(row16_sum(eM.x != kNegInf ? fM * eM.y : 0.f));
   const int qh = bh * a.G + h;

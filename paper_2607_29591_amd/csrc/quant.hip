@@ -126,6 +126,10 @@ struct AppendArgs {
 // A wave per row (keys and values of a token are two); a block has kTokens tokens
 // of one (b, kv head). kAdvance: the block has all of the call's tokens and
 // advances main_len itself; else advance_kernel does, once every block has read it.
+// us at 4, 8, 16, 32 tokens a block: 8 heads of 8 tokens 5.2, 5.0, 5.0, 5.0, of 64
+// 5.1, 6.3, 8.8, 13.8; 256 heads of 16 6.3, 6.8, 7.8, 7.8, of 300 44, 40, 40, 43. A
+// lane with 8 elements of a row in place of 2 took 4.4 us where this takes 3.1 for
+// one token of 8 heads, 37 for 256 heads of 300.
 constexpr int kTokens = 8;
 
 template <typename T, int D, bool kAdvance>

@@ -41,10 +41,15 @@ __device__ __forceinline__ double2 turn(double f, int pos, double scale) {
   return make_double2(scale * (q == 1 || q == 2 ? -cq : cq), scale * (q >= 2 ? -sq : sq));
 }
 
-// (x, y) turned by cs = (A cos a, A sin a).
+// One element of a pair turned by cs = (A cos a, A sin a): x takes -y's part, y
+// takes x's.
+__device__ __forceinline__ double rotate_one(float own, float other, double2 cs, bool first) {
+  const double part = (double)other * cs.y;
+  return fma((double)own, cs.x, first ? -part : part);
+}
 __device__ __forceinline__ void rotate_pair(float x, float y, double2 cs, double& xr, double& yr) {
-  xr = fma((double)x, cs.x, -((double)y * cs.y));
-  yr = fma((double)x, cs.y, (double)y * cs.x);
+  xr = rotate_one(x, y, cs, true);
+  yr = rotate_one(y, x, cs, false);
 }
 
 // 64-bit results rounded once to the row's type. For bf16 by way of 32 bits, which
@@ -95,10 +100,7 @@ struct PairElem {
   __device__ __forceinline__ float rotated(int i, const PairIndex& at, const double2* cs) const {
     const float x = elem(&own, 0), y = elem(&other, 0);
     if (!at.turned(i)) return x;
-    const bool first = at.first(i);
-    double xr, yr;
-    rotate_pair(first ? x : y, first ? y : x, cs[at.pair(i)], xr, yr);
-    return round_to(first ? xr : yr, &own);
+    return round_to(rotate_one(x, y, cs[at.pair(i)], at.first(i)), &own);
   }
 };
 
