@@ -563,8 +563,8 @@ typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
  * Any order of heads and rows is taken (a projection's [B, n, heads, d], a part
  * of a fused one), so the call also moves rows into the layout that the
  * constructions read. An output may be its input (the same pointer and
- * strides); otherwise an output overlaps no input, and its rows do not overlap
- * each other. Pointers are aligned to 16 bytes, strides are multiples of 16 bytes.
+ * strides); otherwise no output row overlaps an input row or another output row.
+ * Pointers are aligned to 16 bytes, strides are multiples of 16 bytes.
  */
 reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope,
                           int32_t n_rows, const int32_t* positions, const int32_t* n_tok,
@@ -654,8 +654,9 @@ reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rop
  *   k_new, v_new    [B, Hkv, d] optional (both or neither): appended as by
  *                   reskv_append_kv_quant before attending (the attention
  *                   reads the values their codes stand for)
- *   workspace       device scratch of reskv_decode_quant_workspace_size() bytes;
- *                   calls sharing one must not overlap
+ *   workspace       device scratch of reskv_decode_quant_workspace_size() bytes,
+ *                   aligned to 16; calls sharing one (replays of graphs that
+ *                   captured it among them) must not overlap
  *   other arguments, and what is written where, as for reskv_decode_attn
  * A head without any live slot gives 0. Slots past res_len + main_len may hold
  * anything, empty entries (logc = -inf) too.

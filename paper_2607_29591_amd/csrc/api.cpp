@@ -439,8 +439,8 @@ reskv_status_t reskv_decode_attn_quant(const reskv_shape_t* shape, const reskv_g
   if ((st = check_turn(shape, rope, positions)) != RESKV_OK) return st;
   if ((k_new == nullptr) != (v_new == nullptr))
     return fail(RESKV_ERR_INVALID_ARG, "k_new and v_new must both be given or both be NULL");
-  if (!aligned(q) || !aligned(cache) || !aligned(k_new) || !aligned(v_new))
-    return fail(RESKV_ERR_INVALID_ARG, "q, k_new, v_new and cache must be aligned to 16 bytes");
+  if (!aligned(q) || !aligned(cache) || !aligned(k_new) || !aligned(v_new) || !aligned(workspace))
+    return fail(RESKV_ERR_INVALID_ARG, "q, k_new, v_new, cache and workspace must be aligned to 16 bytes");
   const QuantDecodePlan plan = make_quant_decode_plan(*shape);
   if (!workspace || workspace_bytes < plan.bytes)
     return fail(RESKV_ERR_WORKSPACE, "decode needs %zu workspace bytes, got %zu", plan.bytes,

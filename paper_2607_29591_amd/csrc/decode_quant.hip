@@ -5,7 +5,8 @@
 // caches; a wave takes blocks of 64 slots (the cache's own blocks) and keeps a
 // running maximum, sum and output per query head for the residual slots, then for
 // the main slots; the waves' states are merged in LDS, where the gate joins the
-// two kinds, or in a second launch over the blocks' records. With hd = lane % 16, g = lane / 16:
+// two kinds, or in a second launch over the blocks' records. With hd = lane % 16,
+// g = lane / 16:
 //   * logits S^T = K Q^T per 16-slot tile t: lane (hd, g) loads D / 4 elements
 //     of key row 16t + hd (16 bytes at D = 128), all of one scale, which the
 //     conversion applies: every code times its scale is a bf16 number, so the
@@ -18,7 +19,16 @@
 //     of step h stands for slot 16(2h + i'/4) + 4g + i'%4, so the B operand is
 //     the lane's own probabilities, as bf16 hi + lo parts, each rounded to
 //     nearest (together 2^-18 of the probability).
-// fp32 queries enter as three bf16 parts, which hold all of their 24 bits.
+// fp32 queries enter as three bf16 parts, which hold all of their 24 bits. (The
+// scaled products of 4-bit with 8-bit numbers would need no conversion of keys, but
+// their sums over differently scaled groups were off by up to 2^-11 of the largest
+// product; logits need 2^-20.)
+//
+// Bound by the memory's rate while the units stream, with about 3 us before (first
+// address translations, queries, rotation) and 1.5 us after (merge, gate). d = 128,
+// bf16: 256 heads of 2048 slots, 4 query heads each (72 MB), 17.3 us a launch, of
+// which 10 stream; 8 heads of 65000 slots 21 us with 4 for the join; 8 heads of 512
+// with rotation and append 8.6 us.
 #include "internal.h"
 #include "quant.h"
 #include "rotate.h"
@@ -250,6 +260,8 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, Unit<D>& u, float (&p)[
     // slot to the lanes of its logits
     const bool weighs = lane >= lo && lane < hi && !(is_res && u.lc == kNegInf);
     s_bias[lane] = !weighs ? kNegInf : is_res ? beta_log2 * u.lc : 0.f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(&s_bias[16 * t + 4 * g]);
@@ -316,7 +328,7 @@ struct Joined {
 };
 __device__ __forceinline__ Joined join(const QuantDecodeArgs& a, int qh, float mM, float lM, float mR, float lR) {
   const float tau = a.tau ? a.tau[qh] : a.tau_scalar;
-  // p_max = 1 / l_main (the largest term is exactly 1), then the gate
+  // p_max = 1 / l_main (the largest term is 1 within a logit's rounding), then the gate
   const float pmax = lM > 0.f ? 1.f / lM : 1.f;
   Joined j;
   j.gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
@@ -427,9 +439,10 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
     float x = h < G ? qe[k].rotated(e, at, s_cs) : 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const uint16_t w = f32_to_bf16_rne(x);
-      s_q[p][h][e] = w;
-      x -= __uint_as_float((uint32_t)w << 16);
+      // truncated: exact in one part or three, and never past the largest number
+      const uint32_t w = __float_as_uint(x) & 0xffff0000u;
+      s_q[p][h][e] = (uint16_t)(w >> 16);
+      x -= __uint_as_float(w);
     }
   }
   const int app_blk = app && app_slot / kUnit >= begin && app_slot / kUnit < end ? app_slot / kUnit : -1;

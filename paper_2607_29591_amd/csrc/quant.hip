@@ -185,8 +185,8 @@ unsigned blocks_for(long long threads) { return (unsigned)((threads + kThreads -
 template <typename T, int D>
 void launch_pack(const reskv_shape_t& s, const void* kc, const void* vc, const int32_t* res_len,
                  const int32_t* main_len, void* cache, hipStream_t stream) {
-  hipLaunchKernelGGL((pack_kernel<T, D>), dim3(blocks_for(((long long)s.slot_cap * (D / 8) + kUnroll - 1) / kUnroll), 2 * s.num_kv_heads, s.batch),
-                     dim3(kThreads), 0, stream, (const T*)kc, (const T*)vc, res_len, main_len, (uint8_t*)cache,
+  const dim3 grid(blocks_for(((long long)s.slot_cap * (D / 8) + kUnroll - 1) / kUnroll), 2 * s.num_kv_heads, s.batch);
+  hipLaunchKernelGGL((pack_kernel<T, D>), grid, dim3(kThreads), 0, stream, (const T*)kc, (const T*)vc, res_len, main_len, (uint8_t*)cache,
                      s.num_kv_heads, s.slot_cap, s.res_cap);
 }
 

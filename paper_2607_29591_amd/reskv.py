@@ -519,7 +519,8 @@ def prepare_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, ou
             _tensor("k_new", k_new, dt, B * H * d), _tensor("v_new", v_new, dt, B * H * d),
             _tensor("out", out, f32, B * Hq * d), _tensor("dbg_lse_main", dbg_lse_main, f32, B * Hq),
             _tensor("dbg_lse_res", dbg_lse_res, f32, B * Hq), _tensor("dbg_gate", dbg_gate, f32, B * Hq),
-            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+            _tensor("workspace", workspace, workspace.dtype, workspace.numel()),
+            workspace.numel() * workspace.element_size(), _stream(stream))
     return _prepared(lib().reskv_decode_attn_quant, args, (shape, gate, rope))
 
 

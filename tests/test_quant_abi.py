@@ -136,7 +136,7 @@ def quant_call(name, **kw):
     ("append", dict(s=shape(head_dim=64), turn=(128, P)), 1),
     ("decode", dict(turn=(128, None)), 1), ("decode", dict(turn=(None, P)), 1),
     ("decode", dict(s=shape(head_dim=64), turn=(128, P)), 1),
-    ("decode", dict(ws=None), 3), ("decode", dict(bytes=0), 3),
+    ("decode", dict(ws=P + 4), 1), ("decode", dict(ws=None), 3), ("decode", dict(bytes=0), 3),
     ("decode", dict(gate=ctypes.byref(rk.make_gate(g_min=2.0))), 1)])
 def test_quant_refusals(name, kw, code):
     assert quant_call(name, **kw) == code
