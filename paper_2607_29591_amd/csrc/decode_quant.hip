@@ -28,7 +28,7 @@
 // address translations, queries, rotation) and 1.5 us after (merge, gate). d = 128,
 // bf16: 256 heads of 2048 slots, 4 query heads each (72 MB), 17.3 us a launch, of
 // which 10 stream; 8 heads of 65000 slots 21 us with 4 for the join; 8 heads of 512
-// with rotation and append 8.6 us.
+// with rotation and append 8.4 us.
 #include "internal.h"
 #include "quant.h"
 #include "rotate.h"
@@ -44,6 +44,10 @@ constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kUnit = 64;  // slots of a cache block
 constexpr int kTiles = kUnit / 16;
+// 16 bytes a row, so that the rows of the heads start in different LDS banks (788
+// thousand conflict clocks a launch of 256 heads without, 1.5 thousand with; uneven
+// caches of 7 query heads 12.4 -> 11.8 us)
+constexpr int kPadQ = 8, kPadAcc = 4;
 constexpr int kMaxParts = 64;  // blocks a head is split over
 
 struct QuantDecodeArgs {
@@ -126,7 +130,7 @@ __device__ __forceinline__ uint4 eight(uint32_t codes, float scale) {
 // Products of the unit's keys and the queries, whose fragments are read from LDS
 // here (kept in registers over the unit they would not fit beside the rest).
 template <int D, int GP, int NP>
-__device__ __forceinline__ void unit_logits(const Unit<D>& u, const uint16_t (*s_q)[GP][D], int hq, int g,
+__device__ __forceinline__ void unit_logits(const Unit<D>& u, const uint16_t (*s_q)[GP][D + kPadQ], int hq, int g,
                                             float (&s)[kTiles][4]) {
   uint4 q[NP][D / 32];
 #pragma unroll
@@ -299,7 +303,8 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, Unit<D>& u, float (&p)[
 }
 
 template <int D, int GP>
-__device__ __forceinline__ void store_state(State<D>& st, float (*acc)[D], float* m, float* l, int hd, int g) {
+__device__ __forceinline__ void store_state(State<D>& st, float (*acc)[D + kPadAcc], float* m, float* l, int hd,
+                                            int g) {
   constexpr int kE = D / 16;
   if (kPaired<GP>) {  // the other half's part (row_ror:8)
 #pragma unroll
@@ -362,12 +367,12 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int hd = lane & 15, g = lane >> 4;
 
-  __shared__ __align__(16) float s_acc[2][kWaves][GP][D];
+  __shared__ __align__(16) float s_acc[2][kWaves][GP][D + kPadAcc];
   __shared__ float s_m[2][kWaves][GP];  // per kind (0 residual, 1 main), per wave
   __shared__ float s_l[2][kWaves][GP];
   __shared__ float s_w[2][kWaves][GP];
   __shared__ __align__(16) float s_bias[kWaves][kUnit];
-  __shared__ __align__(16) uint16_t s_q[NP][GP][D];
+  __shared__ __align__(16) uint16_t s_q[NP][GP][D + kPadQ];
   __shared__ double2 s_cs[64];
 
   // The arguments that the first requests need, read together: left to where
