@@ -48,14 +48,6 @@ __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 w) {
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
-// 16-byte store; kStream: past the caches, for results that are larger than them.
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
-template <bool kStream>
-__device__ __forceinline__ void store16(void* p, u32x4_t v) {
-  if constexpr (kStream) __builtin_nontemporal_store(v, static_cast<u32x4_t*>(p));
-  else *static_cast<u32x4_t*>(p) = v;
-}
-
 // wave64 butterflies over the lanes selected by the xor masks
 __device__ __forceinline__ float wave_xor_max(float v, int mask) {
   return fmaxf(v, __shfl_xor(v, mask, 64));
@@ -109,14 +101,6 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) {
   return x < lo ? lo : (x > hi ? hi : x);
-}
-
-// Lengths of a (b, kv head) cache clamped to its capacities, so corrupt lengths
-// cannot make a kernel read outside it.
-__device__ __forceinline__ void cache_lengths(const int32_t* res_len, const int32_t* main_len,
-                                              int bh, int C, int Rcap, int& r, int& n) {
-  r = clampi(res_len[bh], 0, min(Rcap, C));
-  n = clampi(main_len[bh], 0, C - r);
 }
 
 // ---- 16x16 MFMA tiles over a full row of D elements ------------------------

@@ -87,6 +87,12 @@ struct DecodeArgs {
   float tau_scalar, alpha, g_min;
 };
 
+__device__ __forceinline__ void cache_lengths(const int32_t* res_len, const int32_t* main_len,
+                                              int bh, int C, int Rcap, int& r, int& n) {
+  r = clampi(res_len[bh], 0, min(Rcap, C));
+  n = clampi(main_len[bh], 0, C - r);
+}
+
 // Raw words of one value-row piece (D/16 elements) of one lane.
 template <typename T, int D>
 struct VPiece {

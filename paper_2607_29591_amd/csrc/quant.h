@@ -7,6 +7,22 @@
 namespace reskv {
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
+// Lengths of a (b, kv head) cache clamped to its capacities, so that corrupt
+// lengths cannot make a kernel touch anything outside it.
+__device__ __forceinline__ void cache_lengths(const int32_t* res_len, const int32_t* main_len, int bh, int C, int Rcap,
+                                              int& r, int& n) {
+  r = clampi(res_len[bh], 0, min(Rcap, C));
+  n = clampi(main_len[bh], 0, C - r);
+}
+
+// 16-byte store; kStream: past the caches, for results that are larger than them.
+template <bool kStream>
+__device__ __forceinline__ void store16(void* p, u32x4_t v) {
+  if constexpr (kStream) __builtin_nontemporal_store(v, static_cast<u32x4_t*>(p));
+  else *static_cast<u32x4_t*>(p) = v;
+}
 
 // Offsets in a block of 64 slots.
 template <int D>
