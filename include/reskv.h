@@ -552,7 +552,8 @@ typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
  *   shape           batch, num_q_heads, num_kv_heads, head_dim, dtype
  *                   (slot_cap and res_cap are not used)
  *   rope            plan; rot_dim <= head_dim
- *   n_rows          rows n per sequence and head, >= 0 (a decode step has 1)
+ *   n_rows          rows n per sequence and head, >= 0 (a decode step has 1);
+ *                   B * n at most 2^26
  *   positions       [B, n] int32, device; negative positions turn back
  *   n_tok           [B] int32, device, or NULL: rows t >= n_tok[b] are padding,
  *                   their outputs are left as they were
@@ -596,7 +597,7 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope,
  *   value scales at 66 d:  (((s/4)%4 d/32 + i/32) 4 + s/16) 4 + s%4
  * so that one 16-byte load of a lane (8 bytes at d = 64) brings it what its
  * matrix instructions take. The buffer is aligned to 16 bytes. Up to 65535
- * sequences, 32767 KV heads and 2^30 slots.
+ * sequences, 32767 KV heads and 2^29 slots.
  */
 
 /* Bytes of a 4-bit cache for B, Hkv, d and C of `shape` (0 if invalid). */
@@ -614,7 +615,7 @@ reskv_status_t reskv_pack_quant(const reskv_shape_t* shape, const void* kc, cons
  * reskv_unpack_quant - the values a 4-bit cache stands for, in the shape's type
  * (exact in both types, but for values below a type's normal range).
  *   first_slot      [B*Hkv] int32, device, or NULL (0): the slot of row 0
- *   n_rows          rows to read per (b, kv head), >= 0
+ *   n_rows          rows to read per (b, kv head), 0 .. 2^26
  *   kc, vc          out [B, Hkv, n_rows, d]: row i is slot first_slot + i; rows
  *                   whose slot is not live are left as they were
  */
@@ -629,7 +630,7 @@ reskv_status_t reskv_unpack_quant(const reskv_shape_t* shape, const void* cache,
  *   rope, positions the plan and [B, n_new] int32 (device) positions, or both
  *                   NULL: keys as they are. Rotated keys are rounded to the
  *                   shape's type, exactly as reskv_rope writes them, then coded
- *   n_new           tokens per sequence, >= 0
+ *   n_new           tokens per sequence, 0 .. 2^26
  *   n_tok           [B] int32, device, or NULL: tokens t >= n_tok[b] are
  *                   padding and not appended
  *   k_new, v_new    [B, Hkv, n_new, d]

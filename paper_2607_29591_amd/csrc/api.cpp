@@ -245,6 +245,10 @@ reskv_status_t reskv_append_kv(const reskv_shape_t* shape, const void* k_new, co
   return ok();
 }
 
+// Rows of a call of the rotation, the append or the read-back: a launch has fewer
+// than 2^32 threads along a dimension, and indices of rows stay within 32 bits.
+constexpr int64_t kMaxRows = 1 << 26;
+
 // Row accesses move 16 bytes.
 static bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -338,8 +342,8 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
   if (st != RESKV_OK) return st;
   if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
   if (n_rows == 0) return ok();  // tensors without elements may have no address
-  if ((int64_t)shape->batch * n_rows > INT32_MAX)
-    return fail(RESKV_ERR_UNSUPPORTED, "%d sequences of %d rows are more than 2^31 - 1", shape->batch, n_rows);
+  if (shape->batch * (int64_t)n_rows > kMaxRows)
+    return fail(RESKV_ERR_UNSUPPORTED, "%d sequences of %d rows are more than 2^26", shape->batch, n_rows);
   if (!rope || !positions) return fail(RESKV_ERR_INVALID_ARG, "rope or positions is NULL");
   if ((st = check_rope(shape, rope)) != RESKV_OK) return st;
   if (!q && !q_out && !k && !k_out) return fail(RESKV_ERR_INVALID_ARG, "neither queries nor keys are given");
@@ -357,7 +361,7 @@ static reskv_status_t check_quant_shape(const reskv_shape_t* s) {
   if (st != RESKV_OK) return st;
   if (s->batch > 65535 || s->num_kv_heads > 32767)
     return fail(RESKV_ERR_UNSUPPORTED, "batch %d above 65535 or %d KV heads above 32767", s->batch, s->num_kv_heads);
-  if (s->slot_cap > 1 << 30) return fail(RESKV_ERR_UNSUPPORTED, "slot_cap %d above 2^30", s->slot_cap);
+  if (s->slot_cap > 1 << 29) return fail(RESKV_ERR_UNSUPPORTED, "slot_cap %d above 2^29", s->slot_cap);
   return RESKV_OK;
 }
 
@@ -384,6 +388,7 @@ reskv_status_t reskv_unpack_quant(const reskv_shape_t* shape, const void* cache,
   if (st != RESKV_OK) return st;
   if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
   if (n_rows == 0) return ok();
+  if (n_rows > kMaxRows) return fail(RESKV_ERR_UNSUPPORTED, "n_rows %d above 2^26", n_rows);
   if (!cache || !res_len || !main_len || !kc || !vc) return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
   if (!aligned(kc) || !aligned(vc) || !aligned(cache))
     return fail(RESKV_ERR_INVALID_ARG, "kc, vc and cache must be aligned to 16 bytes");
@@ -407,6 +412,7 @@ reskv_status_t reskv_append_kv_quant(const reskv_shape_t* shape, const reskv_rop
   if (st != RESKV_OK) return st;
   if (n_new < 0) return fail(RESKV_ERR_INVALID_ARG, "n_new %d must be >= 0", n_new);
   if (n_new == 0) return ok();
+  if (n_new > kMaxRows) return fail(RESKV_ERR_UNSUPPORTED, "n_new %d above 2^26", n_new);
   if (!k_new || !v_new || !cache || !res_len || !main_len)
     return fail(RESKV_ERR_INVALID_ARG, "a required pointer is NULL");
   if ((st = check_turn(shape, rope, positions)) != RESKV_OK) return st;

@@ -215,7 +215,7 @@ hipError_t launch_rope(const reskv_shape_t& s, const reskv_rope_t& rope, int n_r
   ra.positions = positions;
   ra.n_tok = n_tok;
   ra.n = n_rows;
-  ra.tokens = s.batch * n_rows;  // within 2^31 - 1
+  ra.tokens = s.batch * n_rows;  // at most 2^26
   if (q) {
     ra.heads[0] = s.num_q_heads;
     ra.src[0] = q; ra.from[0] = *q_at; ra.dst[0] = q_out; ra.to[0] = *q_out_at;

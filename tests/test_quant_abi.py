@@ -82,7 +82,7 @@ def rope_call(s=None, plan=None, n=5, pos=P, q=P, qs=(5120, 640, 128), qo=P << 8
 
 @pytest.mark.parametrize("kw,code", [
     (dict(s=shape(head_dim=96)), 2), (dict(s=shape(dtype=7)), 2), (dict(plan=0), 1), (dict(pos=None), 1),
-    (dict(n=-1), 1), (dict(s=shape(head_dim=64)), 1),                    # the plan turns more than the row has
+    (dict(n=-1), 1), (dict(n=(1 << 25) + 1), 2), (dict(s=shape(head_dim=64)), 1),                    # the plan turns more than the row has
     (dict(plan=rk.Rope(0, 0, 1.0, P)), 1), (dict(plan=rk.Rope(24, 0, 1.0, P)), 1),
     (dict(plan=rk.Rope(64, 2, 1.0, P)), 1), (dict(plan=rk.Rope(64, 0, float("nan"), P)), 1),
     (dict(plan=rk.Rope(64, 0, 1.0, None)), 1),
@@ -131,6 +131,8 @@ def quant_call(name, **kw):
     (n, {x: None}, 1) for n in ("pack", "unpack", "append") for x in ("kc", "vc", "rl", "ml", "cache")] + [
     (n, {x: P + 4}, 1) for n in ("pack", "unpack", "append", "decode") for x in ("kc", "vc", "cache")] + [
     ("decode", {x: None}, 1) for x in ("q", "cache", "logc", "rl", "ml", "out", "kc", "vc", "gate")] + [
+    ("unpack", dict(n=(1 << 26) + 1), 2), ("append", dict(n=(1 << 26) + 1), 2),
+    ("unpack", dict(s=shape(batch=1, slot_cap=(1 << 29) + 1)), 2),
     ("unpack", dict(n=-1), 1), ("append", dict(n=-1), 1), ("decode", dict(q=P + 2), 1),
     ("append", dict(turn=(128, None)), 1), ("append", dict(turn=(None, P)), 1),
     ("append", dict(s=shape(head_dim=64), turn=(128, P)), 1),
