@@ -126,10 +126,13 @@ struct AppendArgs {
 // A wave per row (keys and values of a token are two); a block has kTokens tokens
 // of one (b, kv head). kAdvance: the block has all of the call's tokens and
 // advances main_len itself; else advance_kernel does, once every block has read it.
-// us at 4, 8, 16, 32 tokens a block: 8 heads of 8 tokens 5.2, 5.0, 5.0, 5.0, of 64
-// 5.1, 6.3, 8.8, 13.8; 256 heads of 16 6.3, 6.8, 7.8, 7.8, of 300 44, 40, 40, 43. A
-// lane with 8 elements of a row in place of 2 took 4.4 us where this takes 3.1 for
-// one token of 8 heads, 37 for 256 heads of 300.
+// us at 4, 8, 16, 32 tokens a block, with two of the four waves turning all keys: 8
+// heads of 8 tokens 5.2, 5.0, 5.0, 5.0, of 64 5.1, 6.3, 8.8, 13.8; 256 heads of 16
+// 6.3, 6.8, 7.8, 7.8, of 300 44, 40, 40, 43. With the turns dealt to every wave, at 8:
+// 4.2, 5.5, 6.4, 39.7 (one token of 8 heads 3.1 -> 3.2). A lane with 8 elements of a
+// row in place of 2 took 4.4 us for one token of 8 heads, 37 for 256 heads of 300.
+// Rows requested before the lengths are known: no gain, and slower where n_tok leaves
+// much of a call out.
 constexpr int kTokens = 8;
 
 template <typename T, int D, bool kAdvance>
@@ -141,28 +144,53 @@ __global__ __launch_bounds__(kThreads) void append_quant_kernel(AppendArgs a) {
   cache_lengths(a.res_len, a.main_len, bh, a.C, a.Rcap, r, n);
   const int want = a.n_tok ? clampi(a.n_tok[b], 0, a.n_new) : a.n_new;
   const int take = min(want, a.C - r - n);
-  const int t0 = blockIdx.x * kTokens, rows = 2 * min(kTokens, take - t0);
+  const int t0 = blockIdx.x * kTokens, nt = min(kTokens, take - t0);  // below 1: nothing of this block is taken
   uint8_t* head = a.cache + (size_t)bh * (((size_t)a.C + 63) / 64) * Q::kBytes;
   const int l = min(lane, D / 2 - 1);  // lanes past the row do its last pair again and store nothing
-  __shared__ double2 s_cs[kThreads / 64][64];
-  for (int row = wave; row < rows; row += kThreads / 64) {  // wave-uniform
-    const int t = t0 + (row >> 1);
-    const bool value = row & 1;
-    const T* src = static_cast<const T*>(value ? a.v_new : a.k_new) + ((size_t)bh * a.n_new + t) * D;
-    const PairIndex at(!value && a.positions ? a.rope.rot_dim : 0, a.rope.layout);
-    PairElem<T> x, y;
-    x.load(src, 2 * l, at);
-    y.load(src, 2 * l + 1, at);
-    if (at.rot) {
-      if (lane < at.rot / 2)
-        s_cs[wave][lane] = turn(a.rope.freq[lane], a.positions[(size_t)b * a.n_new + t], a.rope.attn_scale);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+  // Row j of the block: the keys of its nt tokens, then their values, wave by wave, so
+  // that every wave has an equal part of the turns; two of them at once, because one
+  // is a chain of 30 instructions.
+  constexpr int kWaves = kThreads / 64, kRows = 2 * kTokens / kWaves, kKeys = kTokens / kWaves;
+  static_assert(kKeys == 2, "turns of two keys together");
+  const int rot = a.positions ? a.rope.rot_dim : 0;
+  const int keys = rot ? nt - wave : 0;  // of this wave: above 0, above kWaves
+  __shared__ double2 s_cs[kWaves][kKeys][64];
+  PairElem<T> x[kRows], y[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int j = wave + k * kWaves;
+    if (j >= 2 * nt) break;  // wave-uniform
+    const bool value = j >= nt;
+    const PairIndex at(value ? 0 : rot, a.rope.layout);
+    const T* src = static_cast<const T*>(value ? a.v_new : a.k_new) +
+                   ((size_t)bh * a.n_new + t0 + (value ? j - nt : j)) * D;
+    x[k].load(src, 2 * l, at);
+    y[k].load(src, 2 * l + 1, at);
+  }
+  if (keys > 0) {
+    double2* cs = s_cs[wave][0];
+    const int32_t* pos = a.positions + (size_t)b * a.n_new + t0 + wave;
+    const double freq = a.rope.freq[min(lane, rot / 2 - 1)];
+    if (keys > kWaves) {
+      const double2 c0 = turn(freq, pos[0], a.rope.attn_scale), c1 = turn(freq, pos[kWaves], a.rope.attn_scale);
+      cs[lane] = c0;
+      cs[64 + lane] = c1;
+    } else {
+      cs[lane] = turn(freq, pos[0], a.rope.attn_scale);
     }
-    const int slot = r + n + t;
-    store_row_quant<D>(head + (size_t)(slot / 64) * Q::kBytes, slot % 64, value,
-                       x.rotated(2 * l, at, s_cs[wave]), y.rotated(2 * l + 1, at, s_cs[wave]), lane);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int j = wave + k * kWaves;
+    if (j >= 2 * nt) break;
+    const bool value = j >= nt;
+    const PairIndex at(value ? 0 : rot, a.rope.layout);
+    const double2* cs = s_cs[wave][min(k, kKeys - 1)];  // a key is one of the first rows
+    const int slot = r + n + t0 + (value ? j - nt : j);
+    store_row_quant<D>(head + (size_t)(slot / 64) * Q::kBytes, slot % 64, value, x[k].rotated(2 * l, at, cs),
+                       y[k].rotated(2 * l + 1, at, cs), lane);
   }
   if (kAdvance) {
     __syncthreads();  // every wave has read the lengths
