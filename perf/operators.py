@@ -195,7 +195,7 @@ def _quantized(x):
     code = ((y > 0.25).to(torch.uint8) + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5.0))
     value = torch.tensor(E2M1, device=x.device)[code.int()] * _pow2(byte - 127)[..., None]
     value = torch.where(torch.signbit(g), -value, value)
-    return value.flatten(-2), (code + 8 * torch.signbit(g)).to(torch.uint8).flatten(-2), byte.to(torch.uint8)
+    return value.flatten(-2), (code + 8 * torch.signbit(g)).flatten(-2), byte.to(torch.uint8)
 
 
 def _fields(case, cache):
