@@ -401,20 +401,21 @@ def _handles(st):
                  k=zeros(B, H, C, d), v=zeros(B, H, C, d))
         return dict(h, calls=[rk.prepare_pack_quant(shape, st["kc"], st["vc"], *lens, h["cache"]),
                               rk.prepare_unpack_quant(shape, h["cache"], *lens, h["k"], h["v"])])
-    h = dict(k=zeros(B, H, T, d), v=zeros(B, H, T, d), first=(st["res_len"] + st["main_len0"]).contiguous(), calls=[])
+    h = dict(k=zeros(B, H, T, d), v=zeros(B, H, T, d), first=(st["res_len"] + st["main_len0"]).contiguous(), calls=[],
+             cache=st["cache"].to(torch.uint8))   # the calls take bytes
     turn = dict(rope=rope, positions=st["pos"]) if case["rope"] else {}
     if kind == "append":
-        h["calls"].append(rk.prepare_append_kv_quant(shape, st["k_new"], st["v_new"], st["cache"], *lens,
+        h["calls"].append(rk.prepare_append_kv_quant(shape, st["k_new"], st["v_new"], h["cache"], *lens,
                                                      n_tok=st["n_tok"], **turn))
     else:
         gate = rk.make_gate(tau=st["tau"], tau_scalar=TAU, alpha=ALPHA, g_min=G_MIN, beta=BETA)
         h["out"] = torch.zeros((B, Hq, d), dtype=torch.float32, device="cuda")
         h["ws"] = torch.empty(rk.reskv_decode_quant_workspace_size(shape), dtype=torch.uint8, device="cuda")
         new = dict(k_new=st["k_new"][:, :, 0], v_new=st["v_new"][:, :, 0]) if case["append"] else {}
-        h["calls"].append(rk.prepare_decode_attn_quant(shape, gate, st["q"], st["cache"], st["logc"], *lens, h["out"],
+        h["calls"].append(rk.prepare_decode_attn_quant(shape, gate, st["q"], h["cache"], st["logc"], *lens, h["out"],
                                                        h["ws"], **turn, **new))
     if kind == "append" or case["append"]:   # the rows that were appended, read back from the cache
-        h["calls"].append(rk.prepare_unpack_quant(shape, st["cache"], *lens, h["k"], h["v"], first_slot=h["first"]))
+        h["calls"].append(rk.prepare_unpack_quant(shape, h["cache"], *lens, h["k"], h["v"], first_slot=h["first"]))
     return h
 
 
