@@ -338,7 +338,12 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
                           const int32_t* positions, const int32_t* n_tok, const void* q, const reskv_rows_t* q_at,
                           void* q_out, const reskv_rows_t* q_out_at, const void* k, const reskv_rows_t* k_at,
                           void* k_out, const reskv_rows_t* k_out_at, void* stream) {
-  reskv_status_t st = check_shape(shape);
+  reskv_shape_t rows{};  // the shape without the cache's sizes, which a rotation does not use
+  if (shape) {
+    rows = *shape;
+    rows.slot_cap = rows.res_cap = 1;
+  }
+  reskv_status_t st = check_shape(shape ? &rows : nullptr);
   if (st != RESKV_OK) return st;
   if (n_rows < 0) return fail(RESKV_ERR_INVALID_ARG, "n_rows %d must be >= 0", n_rows);
   if (n_rows == 0) return ok();  // tensors without elements may have no address
