@@ -549,8 +549,8 @@ typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
 /*
  * reskv_rope - rotate the rows of queries and keys by their positions.
  *
- *   shape           batch, num_q_heads, num_kv_heads, head_dim, dtype
- *                   (slot_cap and res_cap are not used)
+ *   shape           batch, num_q_heads, num_kv_heads (2^26 heads in all at most),
+ *                   head_dim, dtype (slot_cap and res_cap are not used)
  *   rope            plan; rot_dim <= head_dim
  *   n_rows          rows n per sequence and head, >= 0 (a decode step has 1);
  *                   B * n at most 2^26

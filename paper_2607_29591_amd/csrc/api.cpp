@@ -349,6 +349,10 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
   if (n_rows == 0) return ok();  // tensors without elements may have no address
   if (shape->batch * (int64_t)n_rows > kMaxRows)
     return fail(RESKV_ERR_UNSUPPORTED, "%d sequences of %d rows are more than 2^26", shape->batch, n_rows);
+  // head numbers stay within 32 bits, also those of the few heads past the last that a wave names
+  if ((int64_t)shape->num_q_heads + shape->num_kv_heads > kMaxRows)
+    return fail(RESKV_ERR_UNSUPPORTED, "%d query and %d KV heads are more than 2^26", shape->num_q_heads,
+                shape->num_kv_heads);
   if (!rope || !positions) return fail(RESKV_ERR_INVALID_ARG, "rope or positions is NULL");
   if ((st = check_rope(shape, rope)) != RESKV_OK) return st;
   if (!q && !q_out && !k && !k_out) return fail(RESKV_ERR_INVALID_ARG, "neither queries nor keys are given");

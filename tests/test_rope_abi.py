@@ -27,3 +27,15 @@ def call(s, n, q=None, q_out=None, k=None, k_out=None):
 def test_cache_sizes_are_not_used(kw):
     """slot_cap and res_cap say nothing about a rotation, whatever they hold."""
     assert call(shape(**kw), 0) == 0
+
+
+@pytest.mark.parametrize("hq,hkv,code", [(2 ** 30, 2 ** 30, 2), (2 ** 31 - 1, 2 ** 31 - 1, 2), (2 ** 30, 2 ** 26, 2),
+                                         (2 ** 25 + 1, 2 ** 25 + 1, 2)])
+def test_more_heads_than_a_launch_indexes(hq, hkv, code):
+    """Head numbers are 32-bit, and a wave looks a few heads past its last: 2^26 heads in all are taken. The rows
+    here lie apart from each other, so nothing else refuses the call."""
+    hq -= hq % hkv
+    s = shape(batch=1, num_q_heads=hq, num_kv_heads=hkv, head_dim=64)
+    at = (2 ** 48, 64, 64)
+    assert call(s, 1, q=(P, at), q_out=(P, at)) == code
+    assert "heads" in rk.last_error()
