@@ -290,6 +290,86 @@ static reskv_status_t check_rope(const reskv_shape_t* s, const reskv_rope_t* rop
   return RESKV_OK;
 }
 
+// Rows of one operand, in bytes.
+struct RowSet {
+  int64_t first;
+  int64_t stride[3], extent[3];  // batch, head, row
+};
+
+// Whether a row of a and a row of b have bytes in common: a sum z_0 s_0 + z_1 s_1 + ...
+// of strides that moves a's first row to less than a row's bytes from b's. A stride
+// that both have is one term, their places' difference; else each has its own. Terms
+// are chosen by falling stride, only where what the smaller ones reach, and what is a
+// multiple of all of them, can still come near enough: a few tries where every stride
+// passes what the smaller ones span, as in tensors and slices of tensors.
+enum Overlap { kApart = 0, kCommon = 1, kUntold = 2 };  // kUntold: given up
+struct OverlapSearch {
+  int64_t bytes;  // of a row
+  int terms = 0, tries = 0;
+  int64_t s[6], lo[6], hi[6];
+  int64_t least[7], most[7], unit[7];  // of the sums of terms t and on; what they are multiples of
+
+  void add(int64_t stride, int64_t from, int64_t to) {
+    if (stride == 0 || from == to) return;
+    int t = terms++;
+    for (; t > 0 && s[t - 1] < stride; --t) s[t] = s[t - 1], lo[t] = lo[t - 1], hi[t] = hi[t - 1];
+    s[t] = stride, lo[t] = from, hi[t] = to;
+  }
+  static int64_t down(int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); }  // floor(a / b), b > 0
+  Overlap from(int t, int64_t d) {
+    if (d + most[t] <= -bytes || d + least[t] >= bytes) return kApart;
+    if (t == terms) return kCommon;
+    const int64_t past = d - unit[t] * down(d, unit[t]);
+    if (past >= bytes && unit[t] - past >= bytes) return kApart;
+    if (++tries > 100000) return kUntold;
+    int64_t z0 = -down(bytes - 1 + most[t + 1] + d, s[t]), z1 = down(bytes - 1 - least[t + 1] - d, s[t]);
+    if (z0 < lo[t]) z0 = lo[t];
+    if (z1 > hi[t]) z1 = hi[t];
+    for (int64_t z = z0; z <= z1; ++z) {
+      const Overlap o = from(t + 1, d + z * s[t]);
+      if (o != kApart) return o;
+    }
+    return kApart;
+  }
+};
+
+static Overlap rows_overlap(const RowSet& a, const RowSet& b, int64_t bytes) {
+  OverlapSearch f{bytes};
+  for (int i = 0; i < 3; ++i) {
+    if (a.stride[i] == b.stride[i]) {
+      f.add(a.stride[i], 1 - b.extent[i], a.extent[i] - 1);
+    } else {
+      f.add(a.stride[i], 0, a.extent[i] - 1);
+      f.add(b.stride[i], 1 - b.extent[i], 0);
+    }
+  }
+  f.least[f.terms] = f.most[f.terms] = f.unit[f.terms] = 0;
+  for (int t = f.terms - 1; t >= 0; --t) {
+    f.least[t] = f.least[t + 1] + f.lo[t] * f.s[t];
+    f.most[t] = f.most[t + 1] + f.hi[t] * f.s[t];
+    int64_t x = f.s[t], y = f.unit[t + 1];
+    while (y) {
+      const int64_t m = x % y;
+      x = y;
+      y = m;
+    }
+    f.unit[t] = x;
+  }
+  return f.from(0, a.first - b.first);
+}
+
+static RowSet row_set(const reskv_shape_t* s, int heads, int n, const void* p, const reskv_rows_t* at) {
+  const int64_t e = s->dtype == RESKV_BF16 ? 2 : 4;
+  RowSet r{(int64_t)reinterpret_cast<uintptr_t>(p), {at->batch, at->head, at->row}, {s->batch, heads, n}};
+  for (int i = 0; i < 3; ++i) r.stride[i] = r.extent[i] > 1 ? r.stride[i] * e : 0;  // an unused one may be anything
+  return r;
+}
+
+int reskv_internal_rows_overlap(const int64_t* a, const int64_t* b, int64_t bytes) {
+  return rows_overlap({a[0], {a[1], a[2], a[3]}, {a[4], a[5], a[6]}}, {b[0], {b[1], b[2], b[3]}, {b[4], b[5], b[6]}},
+                      bytes);
+}
+
 // Input and output rows of one kind of heads.
 static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int heads, int n, const void* in,
                                  const reskv_rows_t* from, void* out, const reskv_rows_t* to) {
@@ -299,15 +379,12 @@ static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int h
   if (!aligned(in) || !aligned(out)) return fail(RESKV_ERR_INVALID_ARG, "%s pointers must be aligned to 16 bytes", name);
   const int64_t unit = s->dtype == RESKV_BF16 ? 8 : 4, extent[3] = {s->batch, heads, n};
   const int64_t* st[2] = {&from->batch, &to->batch};
-  int64_t span[2];  // elements from the first row's start to the last row's end
   for (int k = 0; k < 2; ++k) {
-    span[k] = s->head_dim;
     for (int i = 0; i < 3; ++i) {
       if (extent[i] <= 1 && st[k][i] >= 0) continue;  // not used
       if (st[k][i] < 0 || st[k][i] % unit != 0 || st[k][i] > ((int64_t)1 << 48) / (extent[i] - 1))
         return fail(RESKV_ERR_INVALID_ARG, "%s stride %lld is not a multiple of 16 bytes >= 0 within 2^48 elements",
                     name, (long long)st[k][i]);
-      span[k] += (extent[i] - 1) * st[k][i];
     }
   }
   // output rows apart from each other: by rising stride, each passes what the ones before it span
@@ -328,10 +405,13 @@ static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int h
   }
   bool same = in == out;
   for (int i = 0; i < 3; ++i) same = same && (extent[i] <= 1 || st[0][i] == st[1][i]);
-  const uintptr_t e = 16 / unit, i0 = (uintptr_t)in, o0 = (uintptr_t)out;
-  if (!same && i0 < o0 + span[1] * e && o0 < i0 + span[0] * e)
-    return fail(RESKV_ERR_INVALID_ARG, "%s output overlaps its input without being it", name);
-  return RESKV_OK;
+  if (same) return RESKV_OK;
+  switch (rows_overlap(row_set(s, heads, n, in, from), row_set(s, heads, n, out, to), s->head_dim * (16 / unit))) {
+    case kApart: return RESKV_OK;
+    case kCommon: return fail(RESKV_ERR_INVALID_ARG, "%s output overlaps its input without being it", name);
+    case kUntold: break;
+  }
+  return fail(RESKV_ERR_INVALID_ARG, "%s output lies between its input's rows by strides that are not told apart", name);
 }
 
 reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, int32_t n_rows,

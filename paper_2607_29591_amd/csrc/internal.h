@@ -98,6 +98,11 @@ hipError_t launch_decode_quant(const reskv_shape_t& s, const reskv_gate_t& g, co
                                const void* v_new, float* out, float* dbg_lse_main, float* dbg_lse_res,
                                float* dbg_gate, void* workspace, hipStream_t stream);
 
+// Whether rows of two operands of a rotation have bytes in common, for the tests
+// (not part of the C ABI): a, b = first byte, strides in bytes and extents of batch,
+// heads and rows; 0 apart, 1 in common, 2 not told.
+extern "C" int reskv_internal_rows_overlap(const int64_t* a, const int64_t* b, int64_t bytes);
+
 // Which kernels a decode call of these sizes takes, for the tests and the
 // benchmark's labels (not part of the C ABI): entry 0 reskv_decode_attn, 1
 // reskv_decode_branches, 2 reskv_decode_attn_ragged with the workspace its

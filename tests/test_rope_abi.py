@@ -1,6 +1,7 @@
 """Which calls of the rotation are taken and which refused, before any launch (no GPU needed)."""
 
 import ctypes
+import random
 
 import pytest
 
@@ -39,3 +40,61 @@ def test_more_heads_than_a_launch_indexes(hq, hkv, code):
     at = (2 ** 48, 64, 64)
     assert call(s, 1, q=(P, at), q_out=(P, at)) == code
     assert "heads" in rk.last_error()
+
+
+def rows_of(first, stride, extent):
+    return sorted(first + b * stride[0] + h * stride[1] + r * stride[2]
+                  for b in range(extent[0]) for h in range(extent[1]) for r in range(extent[2]))
+
+
+def overlap(a, b, nbytes):
+    """(library's verdict, every row against every row) for operands (first byte, strides, extents)."""
+    fn = rk.lib().reskv_internal_rows_overlap
+    fn.restype, fn.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64]
+    x, y = ((ctypes.c_int64 * 7)(first, *stride, *extent) for first, stride, extent in (a, b))
+    ra, rb = rows_of(*a), rows_of(*b)
+    return fn(x, y, nbytes), int(any(abs(p - q) < nbytes for p in ra for q in rb))
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_overlap_of_rows_is_exact(seed):
+    """Against every pair of rows: operands with strides of their own, of each other, broadcast, and slices of one
+    buffer."""
+    rng = random.Random(seed)
+    said = set()
+    for _ in range(400):
+        n = rng.choice([16, 64, 128])
+        extent = [rng.randint(1, 3), rng.randint(1, 5), rng.randint(1, 5)]
+        order, stride, span = rng.sample(range(3), 3), [0, 0, 0], n * rng.randint(1, 3)
+        for i in order:  # each passes what the ones before it span
+            stride[i] = span + 16 * rng.choice([0, 0, 1, 5, 40])
+            span = stride[i] * extent[i]
+        a = (1 << 20, tuple(stride), tuple(extent))
+        heads = rng.choice([extent[1], 1, rng.randint(1, 6)])
+        other = rng.choice([stride, [stride[0], 2 * stride[1], stride[2]], [stride[0], 0, stride[2]],
+                            [16 * rng.randint(0, 60) for _ in range(3)]])
+        b = ((1 << 20) + 16 * rng.randint(-span // 16 - 8, span // 16 + 8), tuple(other), (extent[0], heads, extent[2]))
+        got, want = overlap(a, b, n)
+        assert got == want, (a, b, n)
+        said.add(got)
+    assert said == {0, 1}
+
+
+def test_overlap_of_slices_at_full_size():
+    """Parts of a fused projection of 65536 tokens, in turns of the same and of another order."""
+    d, heads, tokens = 256, 48, 65536
+    token_major = (0, d, heads * d)
+    fn = rk.lib().reskv_internal_rows_overlap
+    fn.restype, fn.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64]
+
+    def verdict(a, b):
+        return fn(*((ctypes.c_int64 * 7)(x[0], *x[1], *x[2]) for x in (a, b)), d)
+
+    q = ((1 << 32), token_major, (1, 32, tokens))
+    for first, want in ((32, 0), (31, 1), (40, 0), (0, 1)):
+        assert verdict(q, ((1 << 32) + first * d, token_major, (1, 8, tokens))) == want
+    assert verdict(q, ((1 << 32) + 32 * d, (0, 2 * d, heads * d), (1, 8, tokens))) == 0  # every other head
+    assert verdict(q, ((1 << 32) + 31 * d, (0, 2 * d, heads * d), (1, 8, tokens))) == 1
+    head_major = (0, tokens * d, d)
+    assert verdict(q, ((1 << 32) + heads * tokens * d, head_major, (1, 32, tokens))) == 0
+    assert verdict(q, ((1 << 32) + 48 * d, head_major, (1, 32, tokens))) == 1
