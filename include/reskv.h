@@ -565,7 +565,8 @@ typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
  * of a fused one), so the call also moves rows into the layout that the
  * constructions read. An output may be its input (the same pointer and
  * strides); otherwise no output row overlaps an input row or another output row,
- * which the call checks row by row: slices of one buffer may be read and written.
+ * of queries or keys, which the call checks row by row: slices of one buffer may
+ * be read and written.
  * By rising stride, each stride of an output passes what the ones before it span.
  * Pointers are aligned to 16 bytes, strides are multiples of 16 bytes.
  */

@@ -370,6 +370,20 @@ int reskv_internal_rows_overlap(const int64_t* a, const int64_t* b, int64_t byte
                       bytes);
 }
 
+// No row of an output over a row of another operand.
+static reskv_status_t check_apart(const reskv_shape_t* s, const RowSet& out, const char* name, const char* role,
+                                  const RowSet& other, const char* other_name, const char* other_role) {
+  switch (rows_overlap(out, other, s->head_dim * (s->dtype == RESKV_BF16 ? 2 : 4))) {
+    case kApart: return RESKV_OK;
+    case kCommon:
+      return fail(RESKV_ERR_INVALID_ARG, "rows of the %s %s overlap those of the %s %s", name, role, other_name,
+                  other_role);
+    case kUntold: break;
+  }
+  return fail(RESKV_ERR_INVALID_ARG, "the %s %s and the %s %s interleave by strides that are not told apart", name,
+              role, other_name, other_role);
+}
+
 // Input and output rows of one kind of heads.
 static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int heads, int n, const void* in,
                                  const reskv_rows_t* from, void* out, const reskv_rows_t* to) {
@@ -406,12 +420,7 @@ static reskv_status_t check_rows(const reskv_shape_t* s, const char* name, int h
   bool same = in == out;
   for (int i = 0; i < 3; ++i) same = same && (extent[i] <= 1 || st[0][i] == st[1][i]);
   if (same) return RESKV_OK;
-  switch (rows_overlap(row_set(s, heads, n, in, from), row_set(s, heads, n, out, to), s->head_dim * (16 / unit))) {
-    case kApart: return RESKV_OK;
-    case kCommon: return fail(RESKV_ERR_INVALID_ARG, "%s output overlaps its input without being it", name);
-    case kUntold: break;
-  }
-  return fail(RESKV_ERR_INVALID_ARG, "%s output lies between its input's rows by strides that are not told apart", name);
+  return check_apart(s, row_set(s, heads, n, out, to), name, "output", row_set(s, heads, n, in, from), name, "input");
 }
 
 reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, int32_t n_rows,
@@ -438,6 +447,15 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope, 
   if (!q && !q_out && !k && !k_out) return fail(RESKV_ERR_INVALID_ARG, "neither queries nor keys are given");
   if ((st = check_rows(shape, "q", shape->num_q_heads, n_rows, q, q_at, q_out, q_out_at)) != RESKV_OK) return st;
   if ((st = check_rows(shape, "k", shape->num_kv_heads, n_rows, k, k_at, k_out, k_out_at)) != RESKV_OK) return st;
+  if (q && k) {
+    const RowSet q0 = row_set(shape, shape->num_q_heads, n_rows, q, q_at);
+    const RowSet q1 = row_set(shape, shape->num_q_heads, n_rows, q_out, q_out_at);
+    const RowSet k0 = row_set(shape, shape->num_kv_heads, n_rows, k, k_at);
+    const RowSet k1 = row_set(shape, shape->num_kv_heads, n_rows, k_out, k_out_at);
+    if ((st = check_apart(shape, q1, "q", "output", k0, "k", "input")) != RESKV_OK) return st;
+    if ((st = check_apart(shape, k1, "k", "output", q0, "q", "input")) != RESKV_OK) return st;
+    if ((st = check_apart(shape, q1, "q", "output", k1, "k", "output")) != RESKV_OK) return st;
+  }
   hipError_t e = launch_rope(*shape, *rope, n_rows, positions, n_tok, q, q_at, q_out, q_out_at, k, k_at, k_out,
                              k_out_at, (hipStream_t)stream);
   if (e != hipSuccess) return fail(RESKV_ERR_HIP, "rope launch failed: %s", hipGetErrorString(e));

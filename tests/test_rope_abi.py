@@ -98,3 +98,21 @@ def test_overlap_of_slices_at_full_size():
     head_major = (0, tokens * d, d)
     assert verdict(q, ((1 << 32) + heads * tokens * d, head_major, (1, 32, tokens))) == 0
     assert verdict(q, ((1 << 32) + 48 * d, head_major, (1, 32, tokens))) == 1
+
+
+ROWS = (5120, 640, 128)  # of q [2, 8, 5, 128]
+KROWS = (1280, 640, 128)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=(P, ROWS), q_out=(2 * P, ROWS), k=(3 * P, KROWS), k_out=(P, KROWS)),             # keys over the queries
+    dict(q=(P, ROWS), q_out=(2 * P, ROWS), k=(2 * P + 256, KROWS), k_out=(3 * P, KROWS)),   # queries over the keys
+    dict(q=(P, ROWS), q_out=(2 * P, ROWS), k=(3 * P, KROWS), k_out=(2 * P, KROWS)),         # both into one place
+    dict(q=(P, ROWS), q_out=(P, ROWS), k=(P, KROWS), k_out=(P, KROWS)),                     # in place, both the same
+    # a fused projection of 12 heads, keys one head early
+    dict(q=(P, (7680, 128, 1536)), q_out=(P, (7680, 128, 1536)), k=(P + 7 * 256, (7680, 128, 1536)),
+         k_out=(P + 7 * 256, (7680, 128, 1536)))])
+def test_queries_and_keys_overlap(kw):
+    """Queries and keys are rotated side by side: an output over the other's input or output has no order."""
+    assert call(shape(), 5, **kw) == 1
+    assert "overlap" in rk.last_error()
