@@ -167,7 +167,9 @@ def make_shape(batch, num_q_heads, num_kv_heads, head_dim, dtype, slot_cap, res_
 
 
 def make_gate(tau=None, tau_scalar=0.25, alpha=12.0, g_min=0.0, beta=1.0):
-    return Gate(_ptr(tau), tau_scalar, alpha, g_min, beta)
+    g = Gate(_ptr(tau), tau_scalar, alpha, g_min, beta)
+    g.tau_tensor = tau  # keep the thresholds alive with the struct
+    return g
 
 
 def _host_i32(x):
@@ -511,9 +513,9 @@ def prepare_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, ou
                               v_new=None, stream=None):
     """As prepare_rope, for reskv_decode_attn_quant."""
     import torch
-    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     B, Hq, H, d = shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim
     dt, f32 = _dtype(shape), torch.float32
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     args = (ctypes.byref(shape), ctypes.byref(gate), *_turn(shape, rope, positions, 1),
             _tensor("q", q, dt, B * Hq * d), c, _tensor("logc", logc, f32, B * H * shape.res_cap), rl, ml,
             _tensor("k_new", k_new, dt, B * H * d), _tensor("v_new", v_new, dt, B * H * d),
