@@ -515,6 +515,7 @@ def prepare_decode_attn_quant(shape, gate, q, cache, logc, res_len, main_len, ou
     import torch
     B, Hq, H, d = shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim
     dt, f32 = _dtype(shape), torch.float32
+    _tensor("the gate's tau", getattr(gate, "tau_tensor", None), f32, B * Hq)
     c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     args = (ctypes.byref(shape), ctypes.byref(gate), *_turn(shape, rope, positions, 1),
             _tensor("q", q, dt, B * Hq * d), c, _tensor("logc", logc, f32, B * H * shape.res_cap), rl, ml,
