@@ -394,6 +394,13 @@ def _tensor(name, t, dtype, count, contiguous=True):
     return t.data_ptr()
 
 
+def _order(name, t, *size):
+    """Refuse a tensor of as many dimensions as `size` whose dimensions are not these: elements alone do not tell
+    heads from tokens. One with fewer dimensions (a single token, a flat buffer) is told by its elements."""
+    if t is not None and t.dim() == len(size) and tuple(t.shape) != size:
+        raise ValueError(f"{name} must be {list(size)}, got {list(t.shape)}")
+
+
 def _dtype(shape):
     import torch
     return torch.bfloat16 if shape.dtype == RESKV_BF16 else torch.float32
@@ -449,6 +456,8 @@ def _quant_lens(shape, cache, res_len, main_len):
 
 def prepare_pack_quant(shape, kc, vc, res_len, main_len, cache, stream=None):
     """As prepare_rope, for reskv_pack_quant."""
+    for name, x in (("kc", kc), ("vc", vc)):
+        _order(name, x, shape.batch, shape.num_kv_heads, shape.slot_cap, shape.head_dim)
     c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     count = shape.batch * shape.num_kv_heads * shape.slot_cap * shape.head_dim
     args = (ctypes.byref(shape), _tensor("kc", kc, _dtype(shape), count), _tensor("vc", vc, _dtype(shape), count),
@@ -464,8 +473,10 @@ def reskv_pack_quant(shape, kc, vc, res_len, main_len, cache, stream=None):
 def prepare_unpack_quant(shape, cache, res_len, main_len, kc, vc, first_slot=None, stream=None):
     """As prepare_rope, for reskv_unpack_quant."""
     import torch
-    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     pairs, n = shape.batch * shape.num_kv_heads, int(kc.shape[-2])
+    for name, x in (("kc", kc), ("vc", vc)):
+        _order(name, x, shape.batch, shape.num_kv_heads, n, shape.head_dim)
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     args = (ctypes.byref(shape), c, rl, ml, _tensor("first_slot", first_slot, torch.int32, pairs), n,
             _tensor("kc", kc, _dtype(shape), pairs * n * shape.head_dim),
             _tensor("vc", vc, _dtype(shape), pairs * n * shape.head_dim), _stream(stream))
@@ -488,8 +499,12 @@ def prepare_append_kv_quant(shape, k_new, v_new, cache, res_len, main_len, rope=
                             stream=None):
     """As prepare_rope, for reskv_append_kv_quant."""
     import torch
-    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     n = int(k_new.shape[2]) if k_new.dim() == 4 else 1
+    for name, x in (("k_new", k_new), ("v_new", v_new)):
+        _order(name, x, shape.batch, shape.num_kv_heads, n, shape.head_dim)
+    if n > 1:
+        _order("positions", positions, shape.batch, n)
+    c, rl, ml = _quant_lens(shape, cache, res_len, main_len)
     count = shape.batch * shape.num_kv_heads * n * shape.head_dim
     args = (ctypes.byref(shape), *_turn(shape, rope, positions, n), n,
             _tensor("n_tok", n_tok, torch.int32, shape.batch), _tensor("k_new", k_new, _dtype(shape), count),

@@ -43,3 +43,29 @@ def test_thresholds_live_as_long_as_their_gate():
 def test_thresholds_are_checked_as_every_tensor_is(tau, match):
     with pytest.raises(ValueError, match=match):
         decode(rk.make_gate(tau=tau))
+
+
+def rows(*size):
+    return torch.zeros(*size, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("k,v", [((B, 5, H, d), (B, 5, H, d)), ((B, H, 5, d), (B, 5, H, d)), ((B, H, 5, d), (B, H, d, 5)),
+                                 ((H * 5, 1, B, d), (B, H, 5, d))])
+def test_rows_of_another_order_are_refused(k, v):
+    """Tensors of the right number of elements whose heads and tokens lie in another order than [B, Hkv, n, d]."""
+    s, lens = shape(), torch.zeros(B * H, dtype=torch.int32)
+    cache = torch.zeros(rk.reskv_quant_cache_size(s), dtype=torch.uint8)
+    with pytest.raises(ValueError, match=r"must be \[2, 2, \d+, 128\]"):
+        rk.reskv_append_kv_quant(s, rows(*k), rows(*v), cache, lens, lens)
+    with pytest.raises(ValueError, match=r"must be \[2, 2, \d+, 128\]"):
+        rk.reskv_unpack_quant(s, cache, lens, lens, rows(*k), rows(*v))
+    with pytest.raises(ValueError, match=r"must be \[2, 2, 640, 128\]"):
+        rk.reskv_pack_quant(s, *(rows(*(C if x == 5 else x for x in t)) for t in (k, v)), lens, lens, cache)
+
+
+def test_positions_of_another_order_are_refused():
+    s, lens = shape(), torch.zeros(B * H, dtype=torch.int32)
+    with pytest.raises(ValueError, match=r"positions must be \[2, 5\]"):
+        rk.reskv_append_kv_quant(s, rows(B, H, 5, d), rows(B, H, 5, d),
+                                 torch.zeros(rk.reskv_quant_cache_size(s), dtype=torch.uint8), lens, lens,
+                                 rope=rk.make_rope(64), positions=torch.zeros(5, B, dtype=torch.int32))
