@@ -242,6 +242,15 @@ __device__ __forceinline__ void pv_unit(State<D>& st, const Unit<D>& u, const fl
   }
 }
 
+// A logit in 32 bits. Rounded here and never within a later sum: the maximum and the
+// exponents are of the same numbers, so that the largest weight is exactly 1. (With the
+// product fused into the exponent's difference it was off by half of a step of the
+// logit: by 2^64 at 2^31, and a p_max of 0.8 to 1.2 where it is 1 from 2^22 on.)
+__device__ __forceinline__ float scaled(float product, float qk_scale) {
+#pragma clang fp contract(off)
+  return product * qk_scale;
+}
+
 // Online softmax over the unit's slots [lo, hi) of one kind, from the logits'
 // products p, which become the probabilities. Residual slots add beta * log2 count;
 // slots of no weight (outside, empty entries) get zero probability and the least
@@ -257,8 +266,10 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, Unit<D>& u, float (&p)[
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, p[t][i]);
-    top *= qk_scale;
+      for (int i = 0; i < 4; ++i) {
+        p[t][i] = scaled(p[t][i], qk_scale);
+        top = fmaxf(top, p[t][i]);
+      }
   } else {
     // what a slot's logits are moved by (-inf: no weight), from the lane of the
     // slot to the lanes of its logits
@@ -281,14 +292,14 @@ __device__ __forceinline__ void softmax_pv(State<D>& st, Unit<D>& u, float (&p)[
     }
   }
   const float m_new = fmaxf(st.m, rows4_max(top));
-  const float mu = m_new == kNegInf ? 0.f : m_new, scale = full ? qk_scale : 1.f;
+  const float mu = m_new == kNegInf ? 0.f : m_new;
   const float alpha = fast_exp2(st.m - mu);
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[t][i] = fast_exp2(fmaf(p[t][i], scale, -mu));
+      p[t][i] = fast_exp2(p[t][i] - mu);
       sum += p[t][i];
     }
   sum = rows4_sum(sum);
@@ -333,7 +344,7 @@ struct Joined {
 };
 __device__ __forceinline__ Joined join(const QuantDecodeArgs& a, int qh, float mM, float lM, float mR, float lR) {
   const float tau = a.tau ? a.tau[qh] : a.tau_scalar;
-  // p_max = 1 / l_main (the largest term is 1 within a logit's rounding), then the gate
+  // p_max = 1 / l_main (the largest term is exactly 1), then the gate
   const float pmax = lM > 0.f ? 1.f / lM : 1.f;
   Joined j;
   j.gate = fmaxf(a.g_min, 1.f / (1.f + expf(-(tau - pmax) * a.alpha)));
