@@ -428,8 +428,8 @@ __global__ __launch_bounds__(kThreads) void decode_quant_kernel(QuantDecodeArgs 
   Unit<D> u;
   u.load(cache, min(begin + wave, NB - 1), logc, Rcap, lane);
   __builtin_amdgcn_sched_barrier(0);  // no wait for any of them before the last is on its way
-  const int r = clampi(r_raw, 0, min(Rcap, C));  // as cache_lengths
-  int n = clampi(n_raw, 0, C - r);
+  int r, n;
+  clamp_lengths(r_raw, n_raw, C, Rcap, r, n);
   const bool app = kp != nullptr && r + n < C;
   const int app_slot = r + n;
   if (app) n += 1;

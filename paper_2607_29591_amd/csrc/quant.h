@@ -11,10 +11,13 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 // Lengths of a (b, kv head) cache clamped to its capacities, so that corrupt
 // lengths cannot make a kernel touch anything outside it.
+__device__ __forceinline__ void clamp_lengths(int r_raw, int n_raw, int C, int Rcap, int& r, int& n) {
+  r = clampi(r_raw, 0, min(Rcap, C));
+  n = clampi(n_raw, 0, C - r);
+}
 __device__ __forceinline__ void cache_lengths(const int32_t* res_len, const int32_t* main_len, int bh, int C, int Rcap,
                                               int& r, int& n) {
-  r = clampi(res_len[bh], 0, min(Rcap, C));
-  n = clampi(main_len[bh], 0, C - r);
+  clamp_lengths(res_len[bh], main_len[bh], C, Rcap, r, n);
 }
 
 // 16-byte store; kStream: past the caches, for results that are larger than them.
