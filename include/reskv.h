@@ -599,8 +599,9 @@ reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope,
  *   key scales   at 64 d:  ((s%16) d/32 + i/32) 4 + s/16
  *   value scales at 66 d:  (((s/4)%4 d/32 + i/32) 4 + s/16) 4 + s%4
  * so that one 16-byte load of a lane (8 bytes at d = 64) brings it what its
- * matrix instructions take. The buffer is aligned to 16 bytes. Up to 65535
- * sequences, 32767 KV heads and 2^29 slots.
+ * matrix instructions take. The buffer is aligned to 16 bytes, and so are the
+ * tensors of keys, values and queries of these calls. Up to 65535 sequences,
+ * 32767 KV heads and 2^29 slots.
  */
 
 /* Bytes of a 4-bit cache for B, Hkv, d and C of `shape` (0 if invalid). */

@@ -18,17 +18,19 @@
 //     rows 16T + 4g + u, u = 0..3, in one load per T; contraction index 8g + i'
 //     of step h stands for slot 16(2h + i'/4) + 4g + i'%4, so the B operand is
 //     the lane's own probabilities, as bf16 hi + lo parts, each rounded to
-//     nearest (together 2^-18 of the probability).
+//     nearest: for p in [1, 2) the first is off by at most 2^-8, and what is below
+//     2^-8 by at most 2^-17 once it is rounded (2^-17 of the probability).
 // fp32 queries enter as three bf16 parts, which hold all of their 24 bits. (The
 // scaled products of 4-bit with 8-bit numbers would need no conversion of keys, but
 // their sums over differently scaled groups were off by up to 2^-11 of the largest
 // product; logits need 2^-20.)
 //
-// Bound by the memory's rate while the units stream, with about 3 us before (first
-// address translations, queries, rotation) and 1.5 us after (merge, gate). d = 128,
-// bf16: 256 heads of 2048 slots, 4 query heads each (72 MB), 17.3 us a launch, of
-// which 10 stream; 8 heads of 65000 slots 21 us with 4 for the join; 8 heads of 512
-// with rotation and append 8.4 us.
+// Bound by reading the units, with about 3 us before the first one (arguments,
+// lengths, queries, rotation) and 1.5 us after the last (merge, gate), by clocks in the
+// kernel. d = 128, bf16, a launch in a replayed graph: 256 heads of 2048 slots, 4 query
+// heads each (72 MB), 16.8 us where the last-level cache holds them, 18.9 us from memory
+// (3.8 TB/s); 8 heads of 65000 slots 20.5 and 22.1 us, 4 of them the join; 8 heads of
+// 512 with rotation and append 8.4 us.
 #include "internal.h"
 #include "quant.h"
 #include "rotate.h"
@@ -37,9 +39,12 @@ namespace reskv {
 
 namespace {
 
-// Two waves a SIMD. 16 waves of half the registers and units ran 23.6 us where 8 run
-// 17.3 (256 heads of 2048 slots): what a wave does once weighs as much as two units.
-// Requesting a unit ahead changed nothing (17.4).
+// A CU holds one block at d = 128 (151 to 174 registers a wave: two waves a SIMD, or
+// three, where a second block would need four) and two at d = 64 (at most 125
+// registers; one with 16 fp32 heads, whose LDS two would pass). 16 waves of half the
+// registers and units ran 23.6 us where 8 ran 17.3 (d = 128, 256 heads of 2048 slots):
+// what a wave does once weighs as much as two units. Requesting a unit ahead changed
+// nothing (17.4).
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kUnit = 64;  // slots of a cache block
@@ -664,8 +669,8 @@ hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipSt
 // One block per (b, kv head), or its cache blocks dealt to several and their records
 // joined by a second launch. A block takes 512 slots a round (8 waves of 64), about
 // 2 us each while the blocks do not fill the memory's rate; the join and its launch
-// cost 3 us, more once 256 blocks stream at once. Blocks past 256 (one a CU) only
-// wait. Measured at d = 128, bf16, 4 query heads per KV head, every slot live, us one
+// cost 3 us, more once 256 blocks stream at once. Blocks past 256 (one a CU at d = 128)
+// only wait. Measured at d = 128, bf16, 4 query heads per KV head, every slot live, us one
 // block / split so that up to 256 blocks run (lengths uniform in [C/4, C] within 1 us
 // of both):
 //   pairs     C = 1024     1500       2048       2560       4096       8192
@@ -676,7 +681,9 @@ hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipSt
 //   240     11.0/20.4  14.2/22.6  16.7/25.1  18.9/27.6  30.6/38.1  (two or more each)
 // (8 query heads 0.5 to 1 us more on both sides; fp32 rows of 64, 32 pairs: 7.6/8.3,
 // 9.3/8.4, 10.8/8.3, 12.2/8.6, 17.3/8.6, 31.9/11.2.) So a split has to save two
-// rounds, four where the pairs alone fill more than a quarter of the CUs.
+// rounds, four where the pairs alone fill more than a quarter of the CUs. From 129 to
+// 239 pairs and for two blocks a CU (d = 64) nothing was measured: heads stay whole from
+// 129 pairs on, and 256 blocks are the most at both widths.
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   QuantDecodePlan p{};
   p.B = s.batch;

@@ -419,7 +419,8 @@ def _prepared(fn, args, keep):
 
 def prepare_rope(shape, rope, positions, q=None, q_out=None, k=None, k_out=None, n_tok=None, stream=None):
     """Marshal one reskv_rope call once and return a function that issues it (for loops that launch the same
-    calls many times). The caller keeps the tensors alive and unchanged in place."""
+    calls many times). The caller keeps the tensors alive and unchanged in place. The call goes to `stream`, or to the
+    stream that is current now: marshal it on the stream and device on which it will be issued or captured."""
     import torch
     B, d, n = shape.batch, shape.head_dim, int(positions.shape[-1]) if positions.dim() > 1 else 1
     at = []
