@@ -682,8 +682,8 @@ hipError_t launch_gp(const QuantDecodePlan& pl, const QuantDecodeArgs& da, hipSt
 // (8 query heads 0.5 to 1 us more on both sides; fp32 rows of 64, 32 pairs: 7.6/8.3,
 // 9.3/8.4, 10.8/8.3, 12.2/8.6, 17.3/8.6, 31.9/11.2.) So a split has to save two
 // rounds, four where the pairs alone fill more than a quarter of the CUs. From 129 to
-// 239 pairs and for two blocks a CU (d = 64) nothing was measured: heads stay whole from
-// 129 pairs on, and 256 blocks are the most at both widths.
+// 239 pairs, and beyond 256 blocks at d = 64, where a CU holds two, nothing was measured:
+// heads stay whole from 129 pairs on, and 256 blocks are the most at both widths.
 QuantDecodePlan make_quant_decode_plan(const reskv_shape_t& s) {
   QuantDecodePlan p{};
   p.B = s.batch;

@@ -65,8 +65,9 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const T* kc, const T* vc
 // Values of more bytes than the last-level cache holds (256 MB) are stored past the
 // caches: they would have left them before they are read again, and are written
 // faster so (256 x 2304 rows of 128, 2048 of them live, 268 MB: 76 us through the
-// caches, 48 past them, in a replayed graph). Fewer stay where the next call finds them. The lengths
-// are on the device, so the bytes are those of the rows asked for, live or not.
+// caches, 48 past them, in a replayed graph). Fewer stay where the next call finds
+// them. The lengths are on the device, so the bytes are those of the rows asked for,
+// live or not.
 constexpr double kStreamBytes = 256.0 * 1024 * 1024;
 
 template <bool kStream>
