@@ -567,7 +567,8 @@ typedef struct {        /* where the rows of a [B, heads, n, d] tensor are */
  * strides); otherwise no output row overlaps an input row or another output row,
  * of queries or keys, which the call checks row by row: slices of one buffer may
  * be read and written (rows that interleave by strides too odd to be told apart in
- * 100000 tries are refused). By rising stride, each stride of an output passes what the ones before it span.
+ * 100000 tries are refused). By rising stride, each stride of an output passes
+ * what the ones before it span.
  * Pointers are aligned to 16 bytes, strides are multiples of 16 bytes.
  */
 reskv_status_t reskv_rope(const reskv_shape_t* shape, const reskv_rope_t* rope,

@@ -116,3 +116,21 @@ def test_queries_and_keys_overlap(kw):
     """Queries and keys are rotated side by side: an output over the other's input or output has no order."""
     assert call(shape(), 5, **kw) == 1
     assert "overlap" in rk.last_error()
+
+
+def test_overlap_search_ends():
+    """Strides without a common order, apart by a few bytes: given up after a bounded search, never called apart
+    where rows meet."""
+    fn = rk.lib().reskv_internal_rows_overlap
+    fn.restype, fn.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64]
+    verdicts = set()
+    for shift in range(0, 4096, 16):
+        a = (1 << 32, (0, 4096 * 10007, 4096 * 9973), (1, 2000, 2000))
+        b = ((1 << 32) + (1 << 34) + shift, (0, 4096 * 9941, 4096 * 10037), (1, 2000, 2000))
+        verdicts.add((shift < 64 or shift > 4096 - 64,
+                      fn(*((ctypes.c_int64 * 7)(x[0], *x[1], *x[2]) for x in (a, b)), 64)))
+    assert {v for near, v in verdicts if not near} == {0}       # by what all strides are multiples of
+    assert {v for near, v in verdicts if near} <= {1, 2}
+    a = (1 << 32, (0, 16 * 10007, 16 * 9973), (1, 20000, 20000))
+    b = ((1 << 32) + (1 << 31) + 8, (0, 32 * 4970, 32 * 5018), (1, 20000, 20000))
+    assert fn(*((ctypes.c_int64 * 7)(x[0], *x[1], *x[2]) for x in (a, b)), 16) in (1, 2)
